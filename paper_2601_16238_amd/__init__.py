@@ -13,3 +13,5 @@ from .binding import (AttnError, AttnGqaParams, AttnParams, AttnRectParams,  # n
                       attn_fwd_gqa, attn_fwd_rect, attn_fwd_rect_workspace_bytes,
                       attn_probe_atomic_f32, attn_probe_mfma_bf16, attn_probe_stream, attn_version,
                       lib, make_gqa_params, make_params, make_rect_params, status_string)
+from .paged import (AttnPagedParams, attn_fwd_paged, attn_fwd_paged_workspace_bytes,  # noqa: F401
+                    attn_paged_append, make_paged_params)

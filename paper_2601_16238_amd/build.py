@@ -21,6 +21,11 @@ SOURCES = [("attn_api.hip", [], "attn_api.o"),
            ("attn_fwd_wide.hip", ["-DATTN_F16"], "attn_fwd_wide_f16.o"),
            ("attn_fwd.hip", ["-DATTN_F16"], "attn_fwd_f16.o"),
            ("attn_bwd.hip", ["-DATTN_F16"], "attn_bwd_f16.o"),
+           ("attn_paged_api.hip", [], "attn_paged_api.o"),
+           ("attn_paged_fwd.hip", [], "attn_paged_fwd.o"),
+           ("attn_paged_fwd.hip", ["-DATTN_F16"], "attn_paged_fwd_f16.o"),
+           ("attn_paged_append.hip", [], "attn_paged_append.o"),
+           ("attn_paged_append.hip", ["-DATTN_F16"], "attn_paged_append_f16.o"),
            ("rowops.hip", [], "rowops.o"), ("probe.hip", [], "probe.o")]
 # -packed-fp32-ops: never let the compiler form v_pk_*_f32 instructions.
 # -fno-honor-nans (device only): fmaxf lowers to bare v_max/v_max3 without canonicalising

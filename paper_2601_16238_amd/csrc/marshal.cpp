@@ -1,5 +1,5 @@
-// Marshalling of torch tensors into the C ABI of attn.h and rowops.h: checks, output and workspace
-// allocation, and the call, for binding.py, rowops.py and autograd.py.  No arithmetic.  It is native
+// Marshalling of torch tensors into the C ABI of attn.h, attn_paged.h and rowops.h: checks, output and workspace
+// allocation, and the call, for binding.py, paged.py, rowops.py and autograd.py.  No arithmetic.  It is native
 // because the kernels of a short problem take less time than the same checks take in Python (one
 // forward plus backward of two 128-row heads: 45 us of calls for 17 us of kernels), and because an
 // autograd backward runs in the engine's thread on another core, where interpreted code is several
@@ -22,6 +22,7 @@
 #include <vector>
 
 #include "../../include/attn.h"
+#include "../../include/attn_paged.h"
 #include "../../include/rowops.h"
 
 namespace py = pybind11;
@@ -459,6 +460,163 @@ OptTensor fused_attention(const Tensor &q, const Tensor &k, const Tensor &v, dou
     return FusedAttention::apply(q, k, v, scale, causal);
 }
 
+// ---- paged key/value cache -----------------------------------------------------------------------
+
+const int32_t *indexes_of(const Tensor &x, const Tensor &t, int64_t n, const char *name)
+{
+    if (t.scalar_type() != at::kInt || t.device() != x.device() || t.dim() != 1 || t.size(0) != n || !t.is_contiguous())
+        throw py::value_error(std::string(name) + " must be a contiguous int32 GPU tensor of " + std::to_string(n) +
+                              " elements on the tensors' device");
+    return static_cast<const int32_t *>(t.data_ptr());
+}
+
+const Tensor &packed_rows(const Tensor &t, const char *name)
+{
+    if ((t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kHalf) || !t.is_cuda() || t.dim() != 3 ||
+        t.stride(2) != 1)
+        throw py::value_error(std::string(name) + " must be a bf16 or fp16 [T,H,D] GPU tensor with a contiguous D axis");
+    return t;
+}
+
+// An output of the caller's for the rows x, with strides of its own.
+const Tensor &rows_like(const Tensor &x, const Tensor &t, const char *name)
+{
+    packed_rows(t, name);
+    if (t.sizes() != x.sizes() || t.scalar_type() != x.scalar_type() || t.device() != x.device())
+        throw py::value_error(std::string(name) + " must match Q in shape, dtype and device");
+    return t;
+}
+
+// (the stride of an axis of length 1 may hold any value)
+void strides2(const Tensor &t, int64_t &st, int64_t &sh)
+{
+    sh = t.size(1) > 1 ? t.stride(1) : t.size(2);
+    st = t.size(0) > 1 ? t.stride(0) : t.size(1) * sh;
+}
+
+// The batch and the caches of a call on the packed rows x.
+struct Paged {
+    attn_paged_params_t p;
+    const int32_t *page_table, *q_start, *kv_lens;
+    float *k_scale = nullptr, *v_scale = nullptr;
+};
+Paged paged_of(const Tensor &x, int64_t Hq, const Tensor &kc, const Tensor &vc, const Tensor &page_table,
+               const Tensor &q_start, const Tensor &kv_lens, const OptTensor &k_scale, const OptTensor &v_scale)
+{
+    Paged c;
+    require(kc.dim() == 4 && kc.stride(3) == 1 && kc.size(3) == x.size(2) && kc.device() == x.device(),
+            "K_cache must be a [pages,Hkv,page_size,D] tensor with a contiguous D axis on the tensors' device");
+    const bool e4m3 = kc.scalar_type() == at::kFloat8_e4m3fn;
+    require(e4m3 || kc.scalar_type() == x.scalar_type(), "a cache holds the tensors' type or torch.float8_e4m3fn");
+    same_layout(kc, {&vc});
+    require(e4m3 == k_scale.has_value() && e4m3 == v_scale.has_value(),
+            "an e4m3 cache needs k_scale and v_scale, and another takes none");
+    const int64_t pages = kc.size(0), Hkv = kc.size(1);
+    auto scale = [&](const Tensor &t) {
+        require(t.scalar_type() == at::kFloat && t.device() == x.device() && t.is_contiguous() && t.dim() == 2 &&
+                    t.size(0) == pages && t.size(1) == Hkv,
+                "scales must be contiguous fp32 [pages,Hkv] tensors on the tensors' device");
+        return static_cast<float *>(t.data_ptr());
+    };
+    if (e4m3) { c.k_scale = scale(*k_scale); c.v_scale = scale(*v_scale); }
+    const int64_t B = kv_lens.numel();
+    require(page_table.scalar_type() == at::kInt && page_table.device() == x.device() && page_table.dim() == 2 &&
+                page_table.size(0) == B && (page_table.stride(1) == 1 || page_table.size(1) == 1),
+            "page_table must be an int32 [B,width] tensor with contiguous rows on the tensors' device");
+    c.page_table = static_cast<const int32_t *>(page_table.data_ptr());
+    c.kv_lens = indexes_of(x, kv_lens, B, "kv_lens");
+    c.q_start = indexes_of(x, q_start, B + 1, "q_start");
+    const int64_t width = page_table.size(1), row = B > 1 ? page_table.stride(0) : width;
+    for (int64_t n : {x.size(0), B, Hq, Hkv, x.size(2), pages, kc.size(2), width, row})
+        require(n <= INT32_MAX && n >= 0, "a size is out of range");
+    attn_paged_params_contiguous(&c.p, x.size(0), B, Hq, Hkv, x.size(2), pages, kc.size(2), width, 1.0f, 0);
+    c.p.table_stride = row;
+    strides3(kc, c.p.cache_stride_p, c.p.cache_stride_h, c.p.cache_stride_s);
+    return c;
+}
+
+OptTensor attn_paged_append_(const Tensor &k, const Tensor &v, const Tensor &kc, const Tensor &vc,
+                             const Tensor &page_table, const Tensor &q_start, const Tensor &kv_lens,
+                             const OptTensor &cos, const OptTensor &sin, const OptTensor &q, const OptTensor &qrot_in,
+                             const OptTensor &k_scale, const OptTensor &v_scale, const OptStream &stream)
+{
+    packed_rows(k, "K");
+    same_layout(k, {&v});
+    if (q) {
+        packed_rows(*q, "Q");
+        require(q->scalar_type() == k.scalar_type() && q->device() == k.device() && q->size(0) == k.size(0) &&
+                    q->size(2) == k.size(2), "Q must be [T,Hq,D] matching K in T, D, dtype and device");
+    }
+    Paged c = paged_of(k, q ? q->size(1) : k.size(1), kc, vc, page_table, q_start, kv_lens, k_scale, v_scale);
+    require(kc.size(1) == k.size(1), "K and V must have the cache's heads");
+    strides2(k, c.p.kv_stride_t, c.p.kv_stride_h);
+    require(cos.has_value() == sin.has_value(), "cos and sin come together");
+    const float *C = nullptr, *S = nullptr;
+    if (cos) {
+        for (const Tensor *t : {&*cos, &*sin})
+            require(t->scalar_type() == at::kFloat && t->device() == k.device() && t->is_contiguous() && t->dim() == 2 &&
+                        t->sizes() == cos->sizes() && t->size(0) >= page_table.size(1) * kc.size(2) &&
+                        t->size(0) <= INT32_MAX && t->size(1) >= 4 && t->size(1) % 4 == 0 && t->size(1) <= k.size(2) / 2,
+                    "cos/sin tables must be contiguous fp32 [positions, rot/2] tensors on the tensors' device, rot a "
+                    "multiple of 8 up to D, with a row for every position that the page table has room for");
+        c.p.rot = 2 * cos->size(1);
+        c.p.table_rows = cos->size(0);
+        C = static_cast<const float *>(cos->data_ptr());
+        S = static_cast<const float *>(sin->data_ptr());
+    }
+    require(q || !qrot_in, "Q_rot needs Q");
+    const c10::DeviceGuard guard(k.device());
+    OptTensor qrot = qrot_in;
+    if (q) {
+        strides2(*q, c.p.q_stride_t, c.p.q_stride_h);
+        if (qrot) rows_like(*q, *qrot, "Q_rot");
+        else qrot = at::empty(q->sizes(), q->options());
+        strides2(*qrot, c.p.out_stride_t, c.p.out_stride_h);
+    }
+    void *const K = k.data_ptr(), *const V = v.data_ptr(), *const Q = q ? q->data_ptr() : nullptr,
+               *const R = qrot ? qrot->data_ptr() : nullptr, *const KC = kc.data_ptr(), *const VC = vc.data_ptr(),
+               *const st = stream_ptr(stream);
+    check_status(unlocked([&] {
+        return (k.scalar_type() == at::kHalf ? attn_paged_append_f16 : attn_paged_append)(
+            K, V, Q, R, C, S, KC, VC, c.k_scale, c.v_scale, c.page_table, c.q_start, c.kv_lens, &c.p, st);
+    }), "attn_paged_append");
+    return qrot;
+}
+
+std::tuple<Tensor, Tensor> attn_fwd_paged_(const Tensor &q, const Tensor &kc, const Tensor &vc, const Tensor &page_table,
+                                           const Tensor &q_start, const Tensor &kv_lens, double scale, bool causal,
+                                           const OptTensor &k_scale, const OptTensor &v_scale,
+                                           const std::optional<int64_t> &max_q, const OptTensor &o_in,
+                                           const OptTensor &lse_in, const OptTensor &ws_in, bool split,
+                                           const OptStream &stream)
+{
+    packed_rows(q, "Q");
+    Paged c = paged_of(q, q.size(1), kc, vc, page_table, q_start, kv_lens, k_scale, v_scale);
+    strides2(q, c.p.q_stride_t, c.p.q_stride_h);
+    c.p.scale = (float)scale;
+    c.p.causal = causal;
+    if (max_q) c.p.max_q = std::min<int64_t>(std::max<int64_t>(*max_q, -1), q.size(0));
+    const c10::DeviceGuard guard(q.device());
+    const Tensor o = o_in ? rows_like(q, *o_in, "O") : at::empty(q.sizes(), q.options());
+    strides2(o, c.p.out_stride_t, c.p.out_stride_h);
+    if (lse_in) require(lse_in->scalar_type() == at::kFloat && lse_in->is_contiguous() && lse_in->device() == q.device() &&
+                            lse_in->sizes() == q.sizes().slice(0, 2),
+                        "LSE must be a contiguous fp32 [T,Hq] tensor on the tensors' device");
+    const Tensor lse = lse_in ? *lse_in : at::empty(q.sizes().slice(0, 2), q.options().dtype(at::kFloat));
+    Tensor ws;
+    if (ws_in) ws = *ws_in;
+    else if (const size_t need = split ? attn_fwd_paged_workspace_bytes(&c.p) : 0) ws = bytes_on(need, q);
+    const size_t bytes = bytes_of(ws, q);
+    void *const Q = q.data_ptr(), *const KC = kc.data_ptr(), *const VC = vc.data_ptr(), *const O = o.data_ptr(),
+               *const W = data_of(ws), *const st = stream_ptr(stream);
+    float *const L = static_cast<float *>(lse.data_ptr());
+    check_status(unlocked([&] {
+        return (q.scalar_type() == at::kHalf ? attn_fwd_paged_f16 : attn_fwd_paged)(
+            Q, KC, VC, c.k_scale, c.v_scale, c.page_table, c.q_start, c.kv_lens, O, L, W, bytes, &c.p, st);
+    }), "attn_fwd_paged");
+    return {o, lse};
+}
+
 // ---- row-wise kernels ---------------------------------------------------------------------------
 
 const Tensor &rows_of(const Tensor &t, const char *name)
@@ -582,6 +740,8 @@ PYBIND11_MODULE(_marshal, m)
     m.def("attn_bwd_rect", &attn_bwd_rect_);
     m.def("attn_fwd_rope", &attn_fwd_rope_);
     m.def("attn_bwd_rope", &attn_bwd_rope_);
+    m.def("attn_paged_append", &attn_paged_append_);
+    m.def("attn_fwd_paged", &attn_fwd_paged_);
     m.def("fused_attention", &fused_attention);
     m.def("fused_forward", &fused_forward);
     m.def("fused_backward", &fused_backward);
