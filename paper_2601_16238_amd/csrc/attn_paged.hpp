@@ -48,6 +48,18 @@ int launch_paged_append(const PagedAppendArgsT<__bf16> &a, hipStream_t st);
 int launch_paged_append(const PagedAppendArgsT<_Float16> &a, hipStream_t st);
 int launch_paged_fwd(const PagedFwdArgsT<__bf16> &a, hipStream_t st);
 int launch_paged_fwd(const PagedFwdArgsT<_Float16> &a, hipStream_t st);
+int launch_paged_decode(const PagedFwdArgsT<__bf16> &a, int D, int max_rows, int workers, hipStream_t st);
+int launch_paged_decode(const PagedFwdArgsT<_Float16> &a, int D, int max_rows, int workers, hipStream_t st);
+
+// Which kernels a call takes, by what the host knows of the batch: the decoding kernel for the sequences of up to
+// decode_rows rows (new tokens times the query heads of a K/V head; 0: it is not launched), the other for longer ones.
+struct PagedPlan {
+    int kernel_d;     // 64, 128 or 256
+    int decode_rows, decode_workers;  // workers 0: one work-group for each sequence and K/V head
+    bool chunks;
+    size_t bytes;     // workspace
+};
+PagedPlan paged_plan(int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3);
 
 // Rows and keys of a sequence, inside the buffers whatever device memory holds.
 struct PagedSeq {

@@ -1,0 +1,619 @@
+// Attention over the paged cache for sequences of few rows (decoding, speculative decoding): the query heads of a K/V
+// head times the new tokens are at most 16 RB rows, so that K and V are read once and nothing else counts.
+//
+//   S^T = K Q^T (16x16x32 MFMA: keys by rows), p = exp2(c s - m), O^T += V^T P^T.
+//
+// Work: the tiles of TK keys of all sequences and K/V heads, one after the other, are cut into as many equal spans as
+// there are work-groups, whatever the lengths are: the lengths are known on the device only (a captured graph is
+// replayed with others), so each work-group adds them up itself.  A span that begins or ends inside a sequence
+// writes a partial result (m, l, O); attn_paged_merge_kernel joins those.
+//
+// A work-group is NW waves, and each wave works through 32 keys of a tile on its own (nothing is shared but the end of
+// a sequence, where the waves' results are added): K and V reach the wave's own LDS by direct transfers, those of the
+// next tile while this one is computed on, also across the end of a sequence, with no barrier in between.  The 16 keys
+// of a half block lie in one page, whose rows up to the sequence's last key are one buffer resource: slots behind it,
+// pages that are none and columns that do not exist read as zero and fetch nothing.
+//
+// LDS: 16-byte chunk c of row R lies in 64-byte pieces of rows one after the other (four neighbouring lanes of a
+// transfer fetch 64 contiguous bytes), exchanged within 64 bytes by f(R), so that the 16 rows of a K read and the
+// 8 (16) rows of two V transpose reads lie in different banks.
+//
+// e4m3: the codes are converted to the tensors' type exactly; K's scale multiplies the scores of its 16 keys, V's power
+// of two is applied by the conversion and the rest of it to the probabilities before their one rounding.
+#include "attn_paged.hpp"
+
+namespace attn {
+
+typedef elem8 frag;
+__device__ __forceinline__ f32x4 mfma16(frag a, frag b, f32x4 c)
+{
+#ifdef ATTN_F16
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+#else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+#endif
+}
+// Four e4m3 codes times the power of two of `scale`.
+__device__ __forceinline__ elem4 from_e4m3(uint32_t codes, float scale)
+{
+#ifdef ATTN_F16
+    const elem2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, false),
+                hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, true);
+#else
+    const elem2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false),
+                hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true);
+#endif
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
+}
+__device__ __forceinline__ frag from_e4m3(uint32_t lo, uint32_t hi, float scale_lo, float scale_hi)
+{
+    return __builtin_shufflevector(from_e4m3(lo, scale_lo), from_e4m3(hi, scale_hi), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// A value of device memory that no kernel writes while this one runs, by a scalar load.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T *p)
+{
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
+}
+
+template <int D, bool E8>
+struct DecodeCfg {
+    static constexpr int kSize = E8 ? 1 : 2;
+    // (at D = 256 four waves' buffers of 16-bit keys do not fit)
+    static constexpr int kNW = D == 256 && !E8 ? 2 : 4;
+    static constexpr int kThreads = kNW * 64;
+    static constexpr int kTK = kNW * 32;                    // keys of a tile
+    static constexpr int kRows = 1024 / (D * kSize);        // rows of a transfer
+    static constexpr int kPieces = 32 / kRows;              // transfers of a wave's K (V) of a tile
+    static constexpr int kBlock = kRows * 64;               // the next 64 bytes of the rows of a piece
+    static constexpr int kHalf = 16 / kRows * 1024;         // 16 rows further
+    static constexpr int kStage = 2 * kPieces * 1024;       // a wave's K and V of a tile
+    static constexpr int kLds = kNW * 2 * kStage;
+    static constexpr bool kFlip = D == 256 && !E8;          // two rows a piece
+    static constexpr int kSteps = D / 32, kDB = D / 16;
+    static_assert(kStage >= 16 * D * 4, "the waves' results are added in a stage");
+    static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+    // exchange of the chunks of row R, linear in the bits of R
+    __host__ __device__ static constexpr int f(int R)
+    {
+        const int x = R >> 2;
+        return (E8 ? (x & 1) | ((((x >> 1) ^ (x >> 2)) & 1) << 1) : ((x & 1) << 1) | ((x >> 1) & 1)) |
+               (kFlip ? ((R >> 1) & 1) << 2 : 0);
+    }
+    // byte offset of chunk c of row R
+    __host__ __device__ static constexpr int at(int R, int c)
+    {
+        const int x = c ^ f(R);
+        return R / kRows * 1024 + x / 4 * kBlock + R % kRows * 64 + x % 4 * 16;
+    }
+};
+
+// The tiles of the sequences that the kernel takes: those of 1 .. max_rows rows.  (No key: one tile, which has none.)
+__device__ __forceinline__ int decode_tiles(const PagedSeq &s, int G, int max_rows, int TK)
+{
+    return s.n < 1 || (int64_t)s.n * G > max_rows ? 0 : max(1, (s.len + TK - 1) / TK);
+}
+
+// Inclusive sum over a work-group's threads, and over all of them.
+template <int NW>
+__device__ __forceinline__ int block_scan(int v, int *lds, int &all)
+{
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int x = __shfl_up(v, d);
+        if (l >= d) v += x;
+    }
+    __syncthreads();
+    if (l == 63) lds[w] = v;
+    __syncthreads();
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+        if (i < w) v += lds[i];
+        all += lds[i];
+    }
+    return v;
+}
+
+// The tiles of all sequences with one head, and those in front of sequence b_of (if any).
+template <int NW>
+__device__ __forceinline__ int64_t decode_total(const PagedFwdArgs &a, int G, int max_rows, int TK, int *lds,
+                                                int b_of = -1, int64_t *front = nullptr)
+{
+    int64_t total = 0;
+    for (int b0 = 0; b0 < a.b.B; b0 += NW * 64) {
+        const int b = b0 + threadIdx.x;
+        int all, mine = b < a.b.B ? decode_tiles(paged_seq(a.b, b), G, max_rows, TK) : 0;
+        const int sum = block_scan<NW>(mine, lds, all);
+        if (front && b_of >= b0 && b_of < b0 + NW * 64) {
+            __syncthreads();
+            if (b == b_of) lds[0] = sum - mine;
+            __syncthreads();
+            *front = total + lds[0];
+        }
+        total += all;
+    }
+    return total;
+}
+
+// Tiles of a work-group: at least kMinSpan, so that a partial result is little against the keys that it saves the wait for.
+constexpr int kMinSpan = 4;
+__device__ __forceinline__ int64_t decode_span(int64_t tiles, int workers)
+{
+    return max((int64_t)kMinSpan, (tiles + workers - 1) / workers);
+}
+
+// SPLIT: work-groups with spans, partial results in the workspace: [2 spans][rows][D] fp32, then m and l [2][2 spans][rows].
+// Otherwise one work-group for each sequence and K/V head.
+template <int D, int RB, bool E8, bool SPLIT>
+__global__ void __launch_bounds__((DecodeCfg<D, E8>::kThreads))
+attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
+{
+    using C = DecodeCfg<D, E8>;
+    constexpr int NW = C::kNW, TK = C::kTK, R = 16 * RB, KP = C::kPieces;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ int scan[NW];
+    __shared__ float sm[NW][R], sl[NW][R];
+
+    const int tid = threadIdx.x, l = tid & 63, m16 = l & 15, g = l >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int G = a.Hq / a.Hkv, Hkv = a.Hkv, Dr = a.Dr, B = a.b.B;
+
+    // ---- where the span begins
+    struct Unit { int b, h, t, tiles, first, n, len; };  // sequence, K/V head, tile
+    auto load_seq = [&](Unit &u) __attribute__((always_inline)) {
+        u.first = min(max(scalar_load(a.b.q_start + u.b), 0), a.b.T);
+        u.n = max(min(scalar_load(a.b.q_start + u.b + 1), a.b.T) - u.first, 0);
+        u.len = min(max(scalar_load(a.b.kv_lens + u.b), 0), a.b.table_width << a.b.page_shift);
+        u.tiles = u.n < 1 || (int64_t)u.n * G > max_rows ? 0 : max(1, (u.len + TK - 1) / TK);
+    };
+    Unit nx;
+    int64_t left;  // tiles of the span that are not issued yet
+    if constexpr (SPLIT) {
+        const int64_t total = decode_total<NW>(a, G, max_rows, TK, scan);
+        const int64_t span = decode_span(total * Hkv, gridDim.x), begin = blockIdx.x * span;
+        left = min(span, total * Hkv - begin);
+        if (left <= 0) return;
+        // the sequence that tile `begin` lies in
+        int64_t front = 0;
+        int found = -1;
+        for (int b0 = 0; b0 < B && found < 0; b0 += NW * 64) {
+            const int b = b0 + tid;
+            int all, mine = b < B ? decode_tiles(paged_seq(a.b, b), G, max_rows, TK) : 0;
+            const int sum = block_scan<NW>(mine, scan, all);
+            if ((front + all) * Hkv > begin) {
+                __syncthreads();
+                if ((front + sum) * Hkv > begin && (front + sum - mine) * Hkv <= begin) {
+                    scan[0] = b;
+                    scan[1] = sum - mine;
+                }
+                __syncthreads();
+                found = scan[0];
+                front += scan[1];
+            } else {
+                front += all;
+            }
+        }
+        nx.b = __builtin_amdgcn_readfirstlane(found);
+        load_seq(nx);
+        const int in = __builtin_amdgcn_readfirstlane((int)(begin - front * Hkv));
+        nx.h = in / nx.tiles;
+        nx.t = in - nx.h * nx.tiles;
+    } else {
+        nx.b = blockIdx.x / Hkv;
+        nx.h = blockIdx.x % Hkv;
+        nx.t = 0;
+        load_seq(nx);
+        left = nx.tiles;
+        if (left == 0) return;
+    }
+    int todo = __builtin_amdgcn_readfirstlane((int)left);  // tiles that are not computed yet
+
+    // ---- lanes
+    const uint32_t row_bytes = (uint32_t)a.cache_stride_s * C::kSize;
+    constexpr uint32_t kPast = 1u << 31;  // an offset behind every resource
+    // what a lane fetches of a piece: its row, and (exchanged by the piece's f) its chunk
+    const int fetch_row = l / 4 % C::kRows, fetch_chunk = (l / (4 * C::kRows) * 4 + l % 4) ^ C::f(fetch_row);
+    const uint32_t fetch_off = fetch_row * row_bytes;
+    const uint32_t stage0 = lds_address(smem) + w * 2 * C::kStage;
+    const char *const mine = smem + w * 2 * C::kStage;
+    // row reads of K: row m16 of a half, chunk 4 s + g; in the second half f may differ
+    const int k_at[2][2] = {{C::at(m16, g), C::at(m16, 4 + g)}, {C::at(16 + m16, g), C::at(16 + m16, 4 + g)}};
+    // transpose reads of V: column block db of 16, rows 4 g + e (16-bit; the second read is 16 rows further; e4m3: both)
+    int v_at[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (E8) {
+            const int e = m16 >> 1, row = e < 4 ? 4 * g + e : 12 + 4 * g + e;
+            v_at[j] = C::kPieces * 1024 + C::at(row, j) + (l & 1) * 8;
+        } else {
+            v_at[j] = C::kPieces * 1024 + C::at(4 * g + (m16 >> 2), 2 * j + ((l >> 1) & 1)) + (l & 1) * 8;
+        }
+    }
+    // the lane's rows (as columns of S^T): query head and new token
+    int row_q[RB], row_h[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        row_q[rb] = (16 * rb + m16) / G;
+        row_h[rb] = 16 * rb + m16 - row_q[rb] * G;
+    }
+
+    // ---- transfers
+    struct Pages { int id[2]; };           // of the wave's two half blocks of a tile
+    struct Scales { float k[2], v[2]; };
+    auto pages_of = [&](const Unit &u) __attribute__((always_inline)) {
+        Pages p;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const int key = u.t * TK + w * 32 + 16 * hf;
+            p.id[hf] = key < u.len ? scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride +
+                                                 (key >> a.b.page_shift)) : -1;
+        }
+        return p;
+    };
+    auto issue = [&](const Unit &u, const Pages &p, int buf, Scales &sc) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer's last reads are done
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const int key = u.t * TK + w * 32 + 16 * hf;
+            const bool is = a.b.is_page(p.id[hf]);
+            const int rows = is ? min(u.len - key, 16) : 0;
+            const int id = is ? p.id[hf] : 0;
+            const uint32_t bytes = rows > 0 ? (uint32_t)(rows - 1) * row_bytes + Dr * C::kSize : 0;
+            const int64_t off = (id * a.cache_stride_p + u.h * a.cache_stride_h +
+                                 (key & (a.b.page_size() - 1)) * a.cache_stride_s) * C::kSize;
+            const desc_t Kd = make_desc((const char *)a.K_cache + off, bytes),
+                         Vd = make_desc((const char *)a.V_cache + off, bytes);
+            if constexpr (E8) {
+                sc.k[hf] = is ? scalar_load(a.k_scale + (int64_t)id * Hkv + u.h) : 1.f;
+                sc.v[hf] = is ? scalar_load(a.v_scale + (int64_t)id * Hkv + u.h) : 1.f;
+            }
+#pragma unroll
+            for (int n = 0; n < KP / 2; ++n) {
+                const int pc = hf * (KP / 2) + n, chunk = fetch_chunk ^ C::f(pc * C::kRows);
+                const uint32_t voff = chunk * 16 < Dr * C::kSize ? fetch_off + chunk * 16 : kPast;
+                const uint32_t soff = n * C::kRows * row_bytes, lds = stage0 + buf * C::kStage + pc * 1024;
+                dma16_between_nt(Kd, lds, voff, soff);
+                dma16_between_nt(Vd, lds + KP * 1024, voff, soff);
+            }
+        }
+    };
+
+    // ---- a sequence's and head's state
+    frag q[RB][C::kSteps];
+    f32x4 o[RB][C::kDB];
+    float m[RB], lsum[RB];
+    constexpr float kMinusHuge = -1.0e30f;
+    constexpr float kSlack = 8.f;  // probabilities up to 2^8 before the reference maximum moves
+    auto begin_unit = [&](const Unit &u) __attribute__((always_inline)) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            m[rb] = kMinusHuge;
+            lsum[rb] = 0.f;
+#pragma unroll
+            for (int db = 0; db < C::kDB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const bool is = row_q[rb] < u.n;
+            const elem *row = a.Q + (u.first + (is ? row_q[rb] : 0)) * a.q_stride_t +
+                              (u.h * G + (is ? row_h[rb] : 0)) * a.q_stride_h;
+#pragma unroll
+            for (int s = 0; s < C::kSteps; ++s) {
+                // (e4m3: a lane's 16 bytes of K are 16 columns, which make two steps)
+                const int col = E8 ? s / 2 * 64 + g * 16 + s % 2 * 8 : s * 32 + g * 8;
+                q[rb][s] = as_elem8(ld_row16(row, col, Dr));
+            }
+        }
+    };
+    auto compute = [&](const Unit &u, const Pages &p, int buf, const Scales &sc) __attribute__((always_inline)) {
+        const int kb = u.t * TK + w * 32;
+        if (kb >= u.len) return;
+        const char *at = mine + buf * C::kStage;
+        f32x4 s[2][RB];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) s[hf][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < C::kSteps; ++st) {
+                frag k;
+                if constexpr (E8) {
+                    if (st % 2) continue;
+                    const u32x4 c = *(const u32x4 *)(at + k_at[hf][0] + st / 2 * C::kBlock);
+                    const frag k0 = from_e4m3(c.x, c.y, 1.f, 1.f), k1 = from_e4m3(c.z, c.w, 1.f, 1.f);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) {
+                        s[hf][rb] = mfma16(k0, q[rb][st], s[hf][rb]);
+                        s[hf][rb] = mfma16(k1, q[rb][st + 1], s[hf][rb]);
+                    }
+                } else {
+                    k = C::kFlip ? *(const frag *)(at + k_at[hf][st % 2] + st / 2 * 2 * C::kBlock)
+                                 : *(const frag *)(at + k_at[hf][0] + st * C::kBlock);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) s[hf][rb] = mfma16(k, q[rb][st], s[hf][rb]);
+                }
+            }
+        }
+        float c[2] = {a.scale_log2e, a.scale_log2e};
+        if constexpr (E8) {  // (not 0, which a masked score would turn into NaN)
+            c[0] = fmaxf(c[0] * sc.k[0], 1e-38f);
+            c[1] = fmaxf(c[1] * sc.k[1], 1e-38f);
+        }
+        const bool pages = a.b.is_page(p.id[0]) && (kb + 16 >= u.len || a.b.is_page(p.id[1]));
+        if (!pages || kb + 32 > u.len || (a.causal && kb + 32 > u.len - u.n + 1)) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int seen = a.causal ? min(u.len, u.len - u.n + row_q[rb] + 1) : u.len;
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    const int lim = (a.b.is_page(p.id[hf]) ? seen : 0) - kb - 16 * hf - 4 * g;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i >= lim) s[hf][rb][i] = -INFINITY;
+                }
+            }
+        }
+        bool over = false;
+        float top[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float t[2];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+                t[hf] = fmaxf(fmaxf(s[hf][rb][0], s[hf][rb][1]), fmaxf(s[hf][rb][2], s[hf][rb][3])) * c[hf];
+            top[rb] = fmaxf(t[0], t[1]);
+            over |= top[rb] > m[rb] + kSlack;
+        }
+        if (__builtin_amdgcn_ballot_w64(over)) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                float t = xhalf_max(top[rb]);
+                t = fmaxf(t, __shfl_xor(t, 16));
+                const float to = fmaxf(m[rb], t), alpha = fast_exp2(m[rb] - to);
+                m[rb] = to;
+                lsum[rb] *= alpha;
+#pragma unroll
+                for (int db = 0; db < C::kDB; ++db) o[rb][db] *= alpha;
+            }
+        }
+        frag pr[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float e[2][4];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e[hf][i] = fast_exp2(__builtin_fmaf(s[hf][rb][i], c[hf], -m[rb]));
+                    lsum[rb] += e[hf][i];
+                }
+            if constexpr (E8) {
+                // what the conversion leaves of V's scale: in 1 .. 2 (0: 0)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    const uint32_t u32 = __float_as_uint(sc.v[hf]);
+                    const float rest = u32 ? __uint_as_float((u32 & 0x7fffffu) | 0x3f800000u) : 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[hf][i] *= rest;
+                }
+            }
+            pr[rb] = pack8(e[0][0], e[0][1], e[0][2], e[0][3], e[1][0], e[1][1], e[1][2], e[1][3]);
+        }
+#pragma unroll
+        for (int db = 0; db < C::kDB; ++db) {
+            frag v;
+            if constexpr (E8) {
+                typedef int i32x2 __attribute__((ext_vector_type(2)));
+                const i32x2 c8 = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (i32x2 __attribute__((address_space(3))) *)(at + v_at[db % 4] + db / 4 * C::kBlock));
+                v = from_e4m3(c8.x, c8.y, sc.v[0], sc.v[1]);
+            } else {
+                const char *x = C::kFlip ? at + v_at[db % 4] + db / 4 * 2 * C::kBlock
+                                         : at + v_at[db % 2] + db / 2 * C::kBlock;
+                v = join8(lds_read_tr((const elem *)x), lds_read_tr((const elem *)(x + C::kHalf)));
+            }
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) o[rb][db] = mfma16(v, pr[rb], o[rb][db]);
+        }
+    };
+    // The waves' results together, in the stage that has just been worked through.
+    auto end_unit = [&](const Unit &u, bool from_start, bool to_end, int buf) __attribute__((always_inline)) {
+        float ls[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            ls[rb] = xhalf_sum(lsum[rb]);
+            ls[rb] += __shfl_xor(ls[rb], 16);
+            if (g == 0) {
+                sm[w][16 * rb + m16] = m[rb];
+                sl[w][16 * rb + m16] = ls[rb];
+            }
+        }
+        __syncthreads();
+        const int rows = u.n * G;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (from_start ? 1 : 0);
+        float *const part = (float *)a.workspace;
+        float *const part_m = part + 2 * (int64_t)gridDim.x * R * D, *const part_l = part_m + 2 * (int64_t)gridDim.x * R;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            if (16 * rb >= rows) break;
+            const int r = 16 * rb + m16;
+            float top = sm[0][r], all = 0.f;
+#pragma unroll
+            for (int i = 1; i < NW; ++i) top = fmaxf(top, sm[i][r]);
+#pragma unroll
+            for (int i = 0; i < NW; ++i) all += sl[i][r] * fast_exp2(sm[i][r] - top);
+            const float mul = fast_exp2(m[rb] - top);
+            // [16 rows][D] fp32, 16-byte chunks exchanged by the row
+            char *const out = smem + (w * 2 + buf) * C::kStage;
+#pragma unroll
+            for (int db = 0; db < C::kDB; ++db)
+                *(f32x4 *)(out + m16 * (D * 4) + ((4 * db + g) ^ m16) * 16) = o[rb][db] * mul;
+            if (w == 0 && g == 0 && r < rows) {
+                if (from_start && to_end)
+                    a.LSE[(int64_t)(u.first + row_q[rb]) * a.Hq + u.h * G + row_h[rb]] =
+                        all > 0.f ? (top + fast_log2(all)) * kLn2 : -INFINITY;
+                else {
+                    part_m[slot * R + r] = top;
+                    part_l[slot * R + r] = all;
+                }
+            }
+            // the sums of the rows, for the threads that store them
+            __shared__ float inv[16];
+            if (w == 0 && g == 0) inv[m16] = all > 0.f ? 1.f / all : 0.f;
+            __syncthreads();
+            for (int i = tid; i < 16 * (D / 4); i += C::kThreads) {
+                const int row = i / (D / 4), c4 = i % (D / 4), rr = 16 * rb + row;
+                if (rr >= rows || 4 * c4 >= Dr) continue;
+                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < NW; ++k)
+                    x += *(const f32x4 *)(smem + (k * 2 + buf) * C::kStage + row * (D * 4) + (c4 ^ row) * 16);
+                if (from_start && to_end) {
+                    const int t = rr / G, h = rr - t * G;
+                    const float by = inv[row];
+                    *(elem4 *)(a.O + (u.first + t) * a.out_stride_t + (u.h * G + h) * a.out_stride_h + 4 * c4) =
+                        pack4(x[0] * by, x[1] * by, x[2] * by, x[3] * by);
+                } else {
+                    *(f32x4 *)(part + (slot * R + rr) * D + 4 * c4) = x;
+                }
+            }
+            __syncthreads();
+        }
+    };
+
+    auto advance = [&](Unit u) __attribute__((always_inline)) {
+        if (++u.t < u.tiles) return u;
+        u.t = 0;
+        if (++u.h < Hkv) return u;
+        u.h = 0;
+        do {
+            ++u.b;
+            if (u.b < B) load_seq(u);
+        } while (u.b < B && u.tiles == 0);
+        return u;
+    };
+
+    // ---- the span
+    Pages nx_pages = pages_of(nx);
+    Scales sc[2] = {};
+    issue(nx, nx_pages, 0, sc[0]);
+    Unit cur = nx;
+    Pages cur_pages = nx_pages;
+    begin_unit(cur);
+    bool from_start = cur.t == 0;
+    int buf = 0;
+    if (todo > 1) {
+        nx = advance(cur);
+        nx_pages = pages_of(nx);
+    }
+    while (true) {
+        Scales nsc = {};
+        if (todo > 1) {
+            issue(nx, nx_pages, buf ^ 1, nsc);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * KP) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        Unit nn = nx;
+        Pages nn_pages = nx_pages;
+        if (todo > 2) {
+            nn = advance(nx);
+            nn_pages = pages_of(nn);
+        }
+        compute(cur, cur_pages, buf, sc[0]);
+        const bool to_end = cur.t + 1 == cur.tiles;
+        if (to_end || todo == 1) {
+            end_unit(cur, from_start, to_end, buf);
+            if (todo == 1) return;
+            begin_unit(nx);
+            from_start = true;
+        }
+        --todo;
+        cur = nx;
+        cur_pages = nx_pages;
+        nx = nn;
+        nx_pages = nn_pages;
+        sc[0] = nsc;
+        buf ^= 1;
+    }
+}
+
+// The partial results of a sequence and K/V head joined, one work-group for each of its rows.
+template <int D, int RB, bool E8>
+__global__ void __launch_bounds__(256) attn_paged_merge_kernel(const PagedFwdArgs a, const int max_rows,
+                                                               const int workers)
+{
+    constexpr int TK = DecodeCfg<D, E8>::kTK, R = 16 * RB, kCols = D / 4, kPar = 256 / kCols;
+    __shared__ int scan[4];
+    __shared__ f32x4 sum[kPar][kCols];
+    const int G = a.Hq / a.Hkv, b = blockIdx.x / a.Hkv, h = blockIdx.x % a.Hkv, r = blockIdx.y, tid = threadIdx.x;
+    const PagedSeq s = paged_seq(a.b, b);
+    const int tiles = decode_tiles(s, G, max_rows, TK);
+    if (tiles == 0 || r >= s.n * G) return;
+    int64_t front;
+    const int64_t total = decode_total<4>(a, G, max_rows, TK, scan, b, &front);
+    const int64_t span = decode_span(total * a.Hkv, workers), begin = front * a.Hkv + (int64_t)h * tiles;
+    const int w0 = (int)(begin / span), w1 = (int)((begin + tiles - 1) / span);
+    if (w0 == w1) return;  // one work-group had it all
+    const float *part = (const float *)a.workspace;
+    const float *part_m = part + 2 * (int64_t)workers * R * D, *part_l = part_m + 2 * (int64_t)workers * R;
+    auto at = [&](int w) { return (2 * (int64_t)w + (w == w0)) * R + r; };
+    float top = -INFINITY, all = 0.f;
+    for (int w = w0; w <= w1; ++w) top = fmaxf(top, part_m[at(w)]);
+    const int c = tid % kCols, p = tid / kCols;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int w = w0; w <= w1; ++w) all += part_l[at(w)] * fast_exp2(part_m[at(w)] - top);
+    if (4 * c < a.Dr)
+        for (int w = w0 + p; w <= w1; w += kPar) {
+            const int64_t i = at(w);
+            x += *(const f32x4 *)(part + i * D + 4 * c) * fast_exp2(part_m[i] - top);
+        }
+    sum[p][c] = x;
+    __syncthreads();
+    if (p || 4 * c >= a.Dr) return;
+#pragma unroll
+    for (int i = 1; i < kPar; ++i) x += sum[i][c];
+    const float inv = all > 0.f ? 1.f / all : 0.f;
+    const int t = s.first + r / G, hq = h * G + r % G;
+    *(elem4 *)(a.O + t * a.out_stride_t + hq * a.out_stride_h + 4 * c) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    if (c == 0) a.LSE[(int64_t)t * a.Hq + hq] = all > 0.f ? (top + fast_log2(all)) * kLn2 : -INFINITY;
+}
+
+template <int D, int RB, bool E8>
+static int launch_decode_t(const PagedFwdArgs &a, int max_rows, int workers, hipStream_t st)
+{
+    using C = DecodeCfg<D, E8>;
+    const void *kernel = workers ? (const void *)attn_paged_decode_kernel<D, RB, E8, true>
+                                     : (const void *)attn_paged_decode_kernel<D, RB, E8, false>;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds) != hipSuccess) return -1;
+    if (!workers) {
+        hipLaunchKernelGGL((attn_paged_decode_kernel<D, RB, E8, false>), dim3(a.b.B * a.Hkv), dim3(C::kThreads), C::kLds,
+                           st, a, max_rows);
+    } else {
+        hipLaunchKernelGGL((attn_paged_decode_kernel<D, RB, E8, true>), dim3(workers), dim3(C::kThreads), C::kLds, st, a,
+                           max_rows);
+        hipLaunchKernelGGL((attn_paged_merge_kernel<D, RB, E8>), dim3(a.b.B * a.Hkv, max_rows), dim3(256), 0, st, a,
+                           max_rows, workers);
+    }
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+template <int D, bool E8>
+static int launch_decode_d(const PagedFwdArgs &a, int max_rows, int workers, hipStream_t st)
+{
+    if (max_rows <= 16) return launch_decode_t<D, 1, E8>(a, max_rows, workers, st);
+    if (max_rows <= 32) return launch_decode_t<D, 2, E8>(a, max_rows, workers, st);
+    if constexpr (D <= 128) return launch_decode_t<D, 4, E8>(a, max_rows, workers, st);
+    return -1;
+}
+
+int launch_paged_decode(const PagedFwdArgs &a, int D, int max_rows, int workers, hipStream_t st)
+{
+    if (a.k_scale)
+        return D == 64 ? launch_decode_d<64, true>(a, max_rows, workers, st) : D == 128 ? launch_decode_d<128, true>(a, max_rows, workers, st)
+                                                                              : launch_decode_d<256, true>(a, max_rows, workers, st);
+    return D == 64 ? launch_decode_d<64, false>(a, max_rows, workers, st) : D == 128 ? launch_decode_d<128, false>(a, max_rows, workers, st)
+                                                                            : launch_decode_d<256, false>(a, max_rows, workers, st);
+}
+
+}  // namespace attn

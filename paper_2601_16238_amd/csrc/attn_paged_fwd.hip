@@ -4,7 +4,7 @@
 namespace attn {
 
 // One wave for each row and query head: 64 keys at a time, first a score a lane, then four columns a lane.
-__global__ void __launch_bounds__(64) attn_paged_fwd_kernel(const PagedFwdArgs a)
+__global__ void __launch_bounds__(64) attn_paged_fwd_kernel(const PagedFwdArgs a, const int longer)
 {
     __shared__ float probs[64];
     __shared__ int64_t at[64];
@@ -12,7 +12,7 @@ __global__ void __launch_bounds__(64) attn_paged_fwd_kernel(const PagedFwdArgs a
     const int b = paged_seq_of(a.b, t);
     if (b == a.b.B) return;
     const PagedSeq s = paged_seq(a.b, b);
-    if (t < s.first) return;
+    if (t < s.first || (int64_t)s.n * (a.Hq / a.Hkv) <= longer || s.n > a.max_q) return;
     const int seen = a.causal ? min(s.len, s.len - s.n + t - s.first + 1) : s.len;
     const elem *q = a.Q + t * a.q_stride_t + hq * a.q_stride_h;
     auto value = [&](const void *cache, int64_t i, float scale) {
@@ -61,7 +61,11 @@ __global__ void __launch_bounds__(64) attn_paged_fwd_kernel(const PagedFwdArgs a
 
 int launch_paged_fwd(const PagedFwdArgs &a, hipStream_t st)
 {
-    hipLaunchKernelGGL(attn_paged_fwd_kernel, dim3(a.b.T, a.Hq), dim3(64), 0, st, a);
+    const PagedPlan p = paged_plan(a.b.B, a.Hq, a.Hkv, a.Dr, a.max_q, (int64_t)a.b.table_width << a.b.page_shift,
+                                   a.k_scale != nullptr);
+    if (p.decode_rows && launch_paged_decode(a, p.kernel_d, p.decode_rows, a.workspace ? p.decode_workers : 0, st) != 0) return -1;
+    if (p.chunks)
+        hipLaunchKernelGGL(attn_paged_fwd_kernel, dim3(a.b.T, a.Hq), dim3(64), 0, st, a, p.decode_rows);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

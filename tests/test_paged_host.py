@@ -96,6 +96,16 @@ def test_pointers():
         assert call(params(), vs=FAKE) == binding.ATTN_ERR_NULL
 
 
+def test_workspaces():
+    p = params(T=4, B=4, max_q=1, table_width=4096, table_stride=4096)
+    need = attn.lib().attn_fwd_paged_workspace_bytes(ctypes.byref(p))
+    assert need > 0 and need % 256 == 0
+    assert fwd(p, ws=FAKE, ws_bytes=need - 1) == binding.ATTN_ERR_WORKSPACE
+    assert fwd(p, ws=FAKE + 16, ws_bytes=need) == binding.ATTN_ERR_WORKSPACE
+    assert attn.lib().attn_fwd_paged_workspace_bytes(None) == 0
+    assert attn.lib().attn_fwd_paged_workspace_bytes(ctypes.byref(params(D=60))) == 0
+
+
 def test_an_empty_batch_is_nothing_to_do():
     for kw in (dict(T=0), dict(B=0)):
         assert fwd(params(**kw), Q=None, O=None, LSE=None, table=None) == binding.ATTN_OK
