@@ -26,6 +26,8 @@ SOURCES = [("attn_api.hip", [], "attn_api.o"),
            ("attn_paged_fwd.hip", ["-DATTN_F16"], "attn_paged_fwd_f16.o"),
            ("attn_paged_decode.hip", [], "attn_paged_decode.o"),
            ("attn_paged_decode.hip", ["-DATTN_F16"], "attn_paged_decode_f16.o"),
+           ("attn_paged_chunk.hip", [], "attn_paged_chunk.o"),
+           ("attn_paged_chunk.hip", ["-DATTN_F16"], "attn_paged_chunk_f16.o"),
            ("attn_paged_append.hip", [], "attn_paged_append.o"),
            ("attn_paged_append.hip", ["-DATTN_F16"], "attn_paged_append_f16.o"),
            ("rowops.hip", [], "rowops.o"), ("probe.hip", [], "probe.o")]

@@ -51,15 +51,45 @@ int launch_paged_fwd(const PagedFwdArgsT<_Float16> &a, hipStream_t st);
 int launch_paged_decode(const PagedFwdArgsT<__bf16> &a, int D, int max_rows, int workers, hipStream_t st);
 int launch_paged_decode(const PagedFwdArgsT<_Float16> &a, int D, int max_rows, int workers, hipStream_t st);
 
+int launch_paged_chunk(const PagedFwdArgsT<__bf16> &a, int D, int longer, int workers, void *workspace, hipStream_t st);
+int launch_paged_chunk(const PagedFwdArgsT<_Float16> &a, int D, int longer, int workers, void *workspace, hipStream_t st);
+
+// Work in spans: a work-group takes the same number of tiles of keys as every other, from wherever its span begins to
+// wherever it ends.  Of a unit of rows that several have worked on, each leaves a partial result in the workspace: the
+// spans' [2 workers][rows][D] fp32 O relative to a maximum m, in slot 2 w, or 2 w + 1 if it holds the unit's first
+// tile, then m and the sums l, [2 workers][rows] each; and the one that holds the first tile says what is to be joined.
+struct PagedJoin {
+    int first, head, row0, rows;  // packed row and K/V head of the unit; its rows are row0 .. row0+rows-1 of their grid
+    int pieces;                   // workers w, w+1, ..; 0: nothing
+};
+__host__ __device__ constexpr int64_t paged_slots_bytes(int64_t workers, int rows, int D)
+{
+    return 2 * workers * rows * (D + 2) * 4;
+}
+__host__ __device__ constexpr int64_t paged_span_bytes(int64_t workers, int rows, int D)
+{
+    return (paged_slots_bytes(workers, rows, D) + workers * (int64_t)sizeof(PagedJoin) + 255) / 256 * 256;
+}
+template <typename E>
+struct PagedSlots {
+    float *part, *m, *l;
+    PagedJoin *join;
+    __host__ __device__ PagedSlots(void *workspace, int64_t workers, int rows, int D)
+        : part((float *)workspace), m(part + 2 * workers * rows * D), l(m + 2 * workers * rows),
+          join((PagedJoin *)(l + 2 * workers * rows)) {}
+};
+
 // Which kernels a call takes, by what the host knows of the batch: the decoding kernel for the sequences of up to
 // decode_rows rows (new tokens times the query heads of a K/V head; 0: it is not launched), the other for longer ones.
 struct PagedPlan {
     int kernel_d;     // 64, 128 or 256
-    int decode_rows, decode_workers;  // workers 0: one work-group for each sequence and K/V head
+    int decode_rows, decode_workers;  // workers 0: one work-group for each unit of rows
     bool chunks;
-    size_t bytes;     // workspace
+    int chunk_workers;
+    size_t decode_bytes, bytes;       // workspace: the decoding kernel's part, all
 };
-PagedPlan paged_plan(int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3);
+constexpr int kDecodeSpan = 4, kChunkSpan = 4;  // tiles of a span, at least
+PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3);
 
 // Rows and keys of a sequence, inside the buffers whatever device memory holds.
 struct PagedSeq {
@@ -85,6 +115,148 @@ __device__ __forceinline__ int paged_seq_of(const PagedBatch &a, int t)
         if (behind) return b0 + __builtin_ctzll(behind);
     }
     return a.B;
+}
+
+// Inclusive sum over a work-group's threads, and over all of them.
+template <int NW>
+__device__ __forceinline__ int block_scan(int v, int *lds, int &all)
+{
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int x = __shfl_up(v, d);
+        if (l >= d) v += x;
+    }
+    __syncthreads();
+    if (l == 63) lds[w] = v;
+    __syncthreads();
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+        if (i < w) v += lds[i];
+        all += lds[i];
+    }
+    return v;
+}
+
+// The span of worker w of `workers`: `tiles(b)` are those of sequence b with one head, of which there are `heads`.
+// Where the span begins: sequence b, and how many tiles lie in front of that sequence (all heads).
+struct PagedSpan {
+    int64_t begin, front, size;
+    int left, b;  // tiles of the span (0: none)
+};
+template <int NW, typename Tiles>
+__device__ __forceinline__ PagedSpan paged_span(int B, int heads, int w, int workers, int least, int *lds, Tiles tiles)
+{
+    const int tid = threadIdx.x;
+    int64_t total = 0;
+    int mine = 0, sum = 0, all = 0;
+    for (int b0 = 0; b0 < B; b0 += NW * 64) {
+        mine = b0 + tid < B ? tiles(b0 + tid) : 0;
+        sum = block_scan<NW>(mine, lds, all);
+        total += all;
+    }
+    PagedSpan s = {};
+    total *= heads;
+    s.size = max((int64_t)least, (total + workers - 1) / workers);
+    s.begin = w * s.size;
+    const int64_t left = min(s.size, total - s.begin);
+    s.left = __builtin_amdgcn_readfirstlane((int)max(left, (int64_t)0));
+    if (s.left == 0) return s;
+    // (one round: its sums are still there)
+    for (int b0 = 0; b0 < B; b0 += NW * 64) {
+        if (B > NW * 64) {
+            mine = b0 + tid < B ? tiles(b0 + tid) : 0;
+            sum = block_scan<NW>(mine, lds, all);
+        }
+        if ((s.front + all) * heads > s.begin) {
+            __syncthreads();
+            if ((s.front + sum) * heads > s.begin && (s.front + sum - mine) * heads <= s.begin) {
+                lds[0] = b0 + tid;
+                lds[1] = sum - mine;
+            }
+            __syncthreads();
+            s.b = __builtin_amdgcn_readfirstlane(lds[0]);
+            s.front = (s.front + __builtin_amdgcn_readfirstlane(lds[1])) * heads;
+            return s;
+        }
+        s.front += all;
+    }
+    return s;
+}
+
+// A value of device memory that no kernel writes while this one runs, by a scalar load.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T *p)
+{
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
+}
+__device__ __forceinline__ PagedSeq paged_seq_scalar(const PagedBatch &a, int b)
+{
+    PagedSeq s;
+    s.first = min(max(scalar_load(a.q_start + b), 0), a.T);
+    s.n = max(min(scalar_load(a.q_start + b + 1), a.T) - s.first, 0);
+    s.len = min(max(scalar_load(a.kv_lens + b), 0), a.table_width << a.page_shift);
+    return s;
+}
+
+// Four e4m3 codes times the power of two of `scale`.
+__device__ __forceinline__ elem4 from_e4m3(uint32_t codes, float scale)
+{
+#ifdef ATTN_F16
+    const elem2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, false),
+                hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, true);
+#else
+    const elem2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false),
+                hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true);
+#endif
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
+}
+__device__ __forceinline__ elem8 from_e4m3(uint32_t lo, uint32_t hi, float scale_lo, float scale_hi)
+{
+    return __builtin_shufflevector(from_e4m3(lo, scale_lo), from_e4m3(hi, scale_hi), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// What the conversion leaves of a scale, in 1 .. 2; 0 of 0.
+__device__ __forceinline__ float scale_rest(float scale)
+{
+    const uint32_t u = __float_as_uint(scale);
+    return u ? __uint_as_float((u & 0x7fffffu) | 0x3f800000u) : 0.f;
+}
+
+// The partial results of the units that worker blockIdx.x has the first tile of, joined: PAR groups of threads share the
+// pieces of a row, the other threads of the work-group take further rows (grid y).
+template <int D, int PAR>
+__global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedFwdArgs a, const PagedSlots<elem> s, const int R)
+{
+    constexpr int kCols = D / 4, kRows = 256 / kCols / PAR;
+    __shared__ f32x4 sum[PAR > 1 ? PAR : 1][PAR > 1 ? kCols : 1];
+    static_assert(PAR == 1 || kRows == 1, "one row, or one thread for all pieces");
+    const PagedJoin j = s.join[blockIdx.x];
+    const int tid = threadIdx.x, c = tid % kCols, p = PAR > 1 ? tid / kCols : 0;
+    const int r = blockIdx.y * kRows + (PAR > 1 ? 0 : tid / kCols);
+    if (j.pieces == 0 || (PAR > 1 ? r : (int)blockIdx.y * kRows) >= j.rows) return;
+    auto at = [&](int i) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0)) * R + r; };
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, all = 0.f;
+    if (r < j.rows) {
+        for (int i = 0; i < j.pieces; ++i) top = fmaxf(top, s.m[at(i)]);
+        for (int i = 0; i < j.pieces; ++i) all += s.l[at(i)] * fast_exp2(s.m[at(i)] - top);
+        if (4 * c < a.Dr)
+            for (int i = p; i < j.pieces; i += PAR)
+                x += *(const f32x4 *)(s.part + at(i) * D + 4 * c) * fast_exp2(s.m[at(i)] - top);
+    }
+    if constexpr (PAR > 1) {
+        sum[p][c] = x;
+        __syncthreads();
+        if (p) return;
+#pragma unroll
+        for (int i = 1; i < PAR; ++i) x += sum[i][c];
+    }
+    if (r >= j.rows || 4 * c >= a.Dr) return;
+    const float inv = all > 0.f ? 1.f / all : 0.f;
+    const int G = a.Hq / a.Hkv, row = j.row0 + r, t = j.first + row / G, hq = j.head * G + row % G;
+    *(elem4 *)(a.O + t * a.out_stride_t + hq * a.out_stride_h + 4 * c) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    if (c == 0) a.LSE[(int64_t)t * a.Hq + hq] = all > 0.f ? (top + fast_log2(all)) * kLn2 : -INFINITY;
 }
 
 }  // namespace attn

@@ -111,32 +111,6 @@ int fwd_impl(const void *Q, const void *K_cache, const void *V_cache, const floa
 
 }  // namespace
 
-namespace attn {
-
-PagedPlan paged_plan(int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3)
-{
-    PagedPlan p = {};
-    p.kernel_d = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-    const int G = Hq / Hkv, most = p.kernel_d == 256 ? 32 : 64;
-    const int64_t rows = (int64_t)max_q * G;
-    p.chunks = rows > most;
-    // (next to long sequences: those of one new token, or as many as fit beside it)
-    p.decode_rows = !p.chunks ? (int)rows : G <= 16 ? 16 : G <= 32 ? 32 : G <= most ? most : 0;
-    if (!p.decode_rows) return p;
-    const int tile = p.kernel_d == 256 && !e4m3 ? 64 : 128;
-    const int64_t tiles = (keys + tile - 1) / tile;
-    if (tiles > 4) {
-        const int lds = p.kernel_d * (e4m3 ? 1 : 2) * 64 * 2 * (tile / 32), per_cu = 160 * 1024 / (lds + 4096);
-        p.decode_workers = (int)std::min<int64_t>(256 * std::min(per_cu, 2), B * Hkv * ((tiles + 3) / 4));
-        const int R = p.decode_rows <= 16 ? 16 : p.decode_rows <= 32 ? 32 : 64;
-        p.bytes = (size_t)2 * p.decode_workers * R * (p.kernel_d + 2) * sizeof(float);
-        p.bytes = (p.bytes + 255) / 256 * 256;
-    }
-    return p;
-}
-
-}  // namespace attn
-
 extern "C" {
 
 void attn_paged_params_contiguous(attn_paged_params_t *p, int32_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
@@ -176,8 +150,8 @@ size_t attn_fwd_paged_workspace_bytes(const attn_paged_params_t *p)
     if (check_paged(p, false) != ATTN_OK || p->max_q < 1 || p->T == 0 || p->B == 0) return 0;
     // (which cache it is going to be is not known here)
     const int64_t keys = (int64_t)p->table_width * p->page_size;
-    return std::max(attn::paged_plan(p->B, p->Hq, p->Hkv, p->D, p->max_q, keys, false).bytes,
-                    attn::paged_plan(p->B, p->Hq, p->Hkv, p->D, p->max_q, keys, true).bytes);
+    return std::max(attn::paged_plan(p->T, p->B, p->Hq, p->Hkv, p->D, p->max_q, keys, false).bytes,
+                    attn::paged_plan(p->T, p->B, p->Hq, p->Hkv, p->D, p->max_q, keys, true).bytes);
 }
 
 int attn_fwd_paged(const void *Q, const void *K_cache, const void *V_cache, const float *k_scale, const float *v_scale,

@@ -6,7 +6,7 @@
 // Work: the tiles of TK keys of all sequences and K/V heads, one after the other, are cut into as many equal spans as
 // there are work-groups, whatever the lengths are: the lengths are known on the device only (a captured graph is
 // replayed with others), so each work-group adds them up itself.  A span that begins or ends inside a sequence
-// writes a partial result (m, l, O); attn_paged_merge_kernel joins those.
+// writes a partial result (m, l, O); attn_paged_join_kernel joins those.
 //
 // A work-group is NW waves, and each wave works through 32 keys of a tile on its own (nothing is shared but the end of
 // a sequence, where the waves' results are added): K and V reach the wave's own LDS by direct transfers, those of the
@@ -33,30 +33,6 @@ __device__ __forceinline__ f32x4 mfma16(frag a, frag b, f32x4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 #endif
 }
-// Four e4m3 codes times the power of two of `scale`.
-__device__ __forceinline__ elem4 from_e4m3(uint32_t codes, float scale)
-{
-#ifdef ATTN_F16
-    const elem2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, false),
-                hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, true);
-#else
-    const elem2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false),
-                hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true);
-#endif
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
-}
-__device__ __forceinline__ frag from_e4m3(uint32_t lo, uint32_t hi, float scale_lo, float scale_hi)
-{
-    return __builtin_shufflevector(from_e4m3(lo, scale_lo), from_e4m3(hi, scale_hi), 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
-// A value of device memory that no kernel writes while this one runs, by a scalar load.
-template <typename T>
-__device__ __forceinline__ T scalar_load(const T *p)
-{
-    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
-}
-
 template <int D, bool E8>
 struct DecodeCfg {
     static constexpr int kSize = E8 ? 1 : 2;
@@ -89,64 +65,13 @@ struct DecodeCfg {
     }
 };
 
-// The tiles of the sequences that the kernel takes: those of 1 .. max_rows rows.  (No key: one tile, which has none.)
+// The tiles of a sequence that the kernel takes: one of 1 .. max_rows rows.  (No key: one tile, which has none.)
 __device__ __forceinline__ int decode_tiles(const PagedSeq &s, int G, int max_rows, int TK)
 {
     return s.n < 1 || (int64_t)s.n * G > max_rows ? 0 : max(1, (s.len + TK - 1) / TK);
 }
 
-// Inclusive sum over a work-group's threads, and over all of them.
-template <int NW>
-__device__ __forceinline__ int block_scan(int v, int *lds, int &all)
-{
-    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int x = __shfl_up(v, d);
-        if (l >= d) v += x;
-    }
-    __syncthreads();
-    if (l == 63) lds[w] = v;
-    __syncthreads();
-    all = 0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        if (i < w) v += lds[i];
-        all += lds[i];
-    }
-    return v;
-}
-
-// The tiles of all sequences with one head, and those in front of sequence b_of (if any).
-template <int NW>
-__device__ __forceinline__ int64_t decode_total(const PagedFwdArgs &a, int G, int max_rows, int TK, int *lds,
-                                                int b_of = -1, int64_t *front = nullptr)
-{
-    int64_t total = 0;
-    for (int b0 = 0; b0 < a.b.B; b0 += NW * 64) {
-        const int b = b0 + threadIdx.x;
-        int all, mine = b < a.b.B ? decode_tiles(paged_seq(a.b, b), G, max_rows, TK) : 0;
-        const int sum = block_scan<NW>(mine, lds, all);
-        if (front && b_of >= b0 && b_of < b0 + NW * 64) {
-            __syncthreads();
-            if (b == b_of) lds[0] = sum - mine;
-            __syncthreads();
-            *front = total + lds[0];
-        }
-        total += all;
-    }
-    return total;
-}
-
-// Tiles of a work-group: at least kMinSpan, so that a partial result is little against the keys that it saves the wait for.
-constexpr int kMinSpan = 4;
-__device__ __forceinline__ int64_t decode_span(int64_t tiles, int workers)
-{
-    return max((int64_t)kMinSpan, (tiles + workers - 1) / workers);
-}
-
-// SPLIT: work-groups with spans, partial results in the workspace: [2 spans][rows][D] fp32, then m and l [2][2 spans][rows].
-// Otherwise one work-group for each sequence and K/V head.
+// SPLIT: work-groups with spans, partial results in the workspace.  Otherwise one work-group for each sequence and K/V head.
 template <int D, int RB, bool E8, bool SPLIT>
 __global__ void __launch_bounds__((DecodeCfg<D, E8>::kThreads))
 attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
@@ -160,45 +85,29 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
     const int tid = threadIdx.x, l = tid & 63, m16 = l & 15, g = l >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = a.Hq / a.Hkv, Hkv = a.Hkv, Dr = a.Dr, B = a.b.B;
+    const PagedSlots<elem> slots(a.workspace, gridDim.x, R, D);
 
     // ---- where the span begins
     struct Unit { int b, h, t, tiles, first, n, len; };  // sequence, K/V head, tile
     auto load_seq = [&](Unit &u) __attribute__((always_inline)) {
-        u.first = min(max(scalar_load(a.b.q_start + u.b), 0), a.b.T);
-        u.n = max(min(scalar_load(a.b.q_start + u.b + 1), a.b.T) - u.first, 0);
-        u.len = min(max(scalar_load(a.b.kv_lens + u.b), 0), a.b.table_width << a.b.page_shift);
-        u.tiles = u.n < 1 || (int64_t)u.n * G > max_rows ? 0 : max(1, (u.len + TK - 1) / TK);
+        const PagedSeq s = paged_seq_scalar(a.b, u.b);
+        u.first = s.first;
+        u.n = s.n;
+        u.len = s.len;
+        u.tiles = decode_tiles(s, G, max_rows, TK);
     };
     Unit nx;
-    int64_t left;  // tiles of the span that are not issued yet
+    int todo;  // tiles of the span that are not computed yet
+    PagedSpan span = {};
     if constexpr (SPLIT) {
-        const int64_t total = decode_total<NW>(a, G, max_rows, TK, scan);
-        const int64_t span = decode_span(total * Hkv, gridDim.x), begin = blockIdx.x * span;
-        left = min(span, total * Hkv - begin);
-        if (left <= 0) return;
-        // the sequence that tile `begin` lies in
-        int64_t front = 0;
-        int found = -1;
-        for (int b0 = 0; b0 < B && found < 0; b0 += NW * 64) {
-            const int b = b0 + tid;
-            int all, mine = b < B ? decode_tiles(paged_seq(a.b, b), G, max_rows, TK) : 0;
-            const int sum = block_scan<NW>(mine, scan, all);
-            if ((front + all) * Hkv > begin) {
-                __syncthreads();
-                if ((front + sum) * Hkv > begin && (front + sum - mine) * Hkv <= begin) {
-                    scan[0] = b;
-                    scan[1] = sum - mine;
-                }
-                __syncthreads();
-                found = scan[0];
-                front += scan[1];
-            } else {
-                front += all;
-            }
-        }
-        nx.b = __builtin_amdgcn_readfirstlane(found);
+        span = paged_span<NW>(B, Hkv, blockIdx.x, gridDim.x, kDecodeSpan, scan,
+                              [&](int b) { return decode_tiles(paged_seq(a.b, b), G, max_rows, TK); });
+        todo = span.left;
+        if (tid == 0) slots.join[blockIdx.x].pieces = 0;
+        if (todo == 0) return;
+        nx.b = span.b;
         load_seq(nx);
-        const int in = __builtin_amdgcn_readfirstlane((int)(begin - front * Hkv));
+        const int in = __builtin_amdgcn_readfirstlane((int)(span.begin - span.front));
         nx.h = in / nx.tiles;
         nx.t = in - nx.h * nx.tiles;
     } else {
@@ -206,10 +115,9 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         nx.h = blockIdx.x % Hkv;
         nx.t = 0;
         load_seq(nx);
-        left = nx.tiles;
-        if (left == 0) return;
+        todo = nx.tiles;
+        if (todo == 0) return;
     }
-    int todo = __builtin_amdgcn_readfirstlane((int)left);  // tiles that are not computed yet
 
     // ---- lanes
     const uint32_t row_bytes = (uint32_t)a.cache_stride_s * C::kSize;
@@ -391,8 +299,7 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
                 // what the conversion leaves of V's scale: in 1 .. 2 (0: 0)
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
-                    const uint32_t u32 = __float_as_uint(sc.v[hf]);
-                    const float rest = u32 ? __uint_as_float((u32 & 0x7fffffu) | 0x3f800000u) : 0.f;
+                    const float rest = scale_rest(sc.v[hf]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) e[hf][i] *= rest;
                 }
@@ -431,8 +338,11 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         __syncthreads();
         const int rows = u.n * G;
         const int64_t slot = 2 * (int64_t)blockIdx.x + (from_start ? 1 : 0);
-        float *const part = (float *)a.workspace;
-        float *const part_m = part + 2 * (int64_t)gridDim.x * R * D, *const part_l = part_m + 2 * (int64_t)gridDim.x * R;
+        if (SPLIT && from_start && !to_end && tid == 0) {
+            // the unit's last tile lies u.tiles - u.t - 1 behind this one, the span's last
+            const int64_t last = span.begin + span.left - 1 + (u.tiles - 1 - u.t);
+            slots.join[blockIdx.x] = PagedJoin{u.first, u.h, 0, rows, (int)(last / span.size) - (int)blockIdx.x + 1};
+        }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             if (16 * rb >= rows) break;
@@ -453,8 +363,8 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
                     a.LSE[(int64_t)(u.first + row_q[rb]) * a.Hq + u.h * G + row_h[rb]] =
                         all > 0.f ? (top + fast_log2(all)) * kLn2 : -INFINITY;
                 else {
-                    part_m[slot * R + r] = top;
-                    part_l[slot * R + r] = all;
+                    slots.m[slot * R + r] = top;
+                    slots.l[slot * R + r] = all;
                 }
             }
             // the sums of the rows, for the threads that store them
@@ -474,7 +384,7 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
                     *(elem4 *)(a.O + (u.first + t) * a.out_stride_t + (u.h * G + h) * a.out_stride_h + 4 * c4) =
                         pack4(x[0] * by, x[1] * by, x[2] * by, x[3] * by);
                 } else {
-                    *(f32x4 *)(part + (slot * R + rr) * D + 4 * c4) = x;
+                    *(f32x4 *)(slots.part + (slot * R + rr) * D + 4 * c4) = x;
                 }
             }
             __syncthreads();
@@ -538,47 +448,6 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
     }
 }
 
-// The partial results of a sequence and K/V head joined, one work-group for each of its rows.
-template <int D, int RB, bool E8>
-__global__ void __launch_bounds__(256) attn_paged_merge_kernel(const PagedFwdArgs a, const int max_rows,
-                                                               const int workers)
-{
-    constexpr int TK = DecodeCfg<D, E8>::kTK, R = 16 * RB, kCols = D / 4, kPar = 256 / kCols;
-    __shared__ int scan[4];
-    __shared__ f32x4 sum[kPar][kCols];
-    const int G = a.Hq / a.Hkv, b = blockIdx.x / a.Hkv, h = blockIdx.x % a.Hkv, r = blockIdx.y, tid = threadIdx.x;
-    const PagedSeq s = paged_seq(a.b, b);
-    const int tiles = decode_tiles(s, G, max_rows, TK);
-    if (tiles == 0 || r >= s.n * G) return;
-    int64_t front;
-    const int64_t total = decode_total<4>(a, G, max_rows, TK, scan, b, &front);
-    const int64_t span = decode_span(total * a.Hkv, workers), begin = front * a.Hkv + (int64_t)h * tiles;
-    const int w0 = (int)(begin / span), w1 = (int)((begin + tiles - 1) / span);
-    if (w0 == w1) return;  // one work-group had it all
-    const float *part = (const float *)a.workspace;
-    const float *part_m = part + 2 * (int64_t)workers * R * D, *part_l = part_m + 2 * (int64_t)workers * R;
-    auto at = [&](int w) { return (2 * (int64_t)w + (w == w0)) * R + r; };
-    float top = -INFINITY, all = 0.f;
-    for (int w = w0; w <= w1; ++w) top = fmaxf(top, part_m[at(w)]);
-    const int c = tid % kCols, p = tid / kCols;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int w = w0; w <= w1; ++w) all += part_l[at(w)] * fast_exp2(part_m[at(w)] - top);
-    if (4 * c < a.Dr)
-        for (int w = w0 + p; w <= w1; w += kPar) {
-            const int64_t i = at(w);
-            x += *(const f32x4 *)(part + i * D + 4 * c) * fast_exp2(part_m[i] - top);
-        }
-    sum[p][c] = x;
-    __syncthreads();
-    if (p || 4 * c >= a.Dr) return;
-#pragma unroll
-    for (int i = 1; i < kPar; ++i) x += sum[i][c];
-    const float inv = all > 0.f ? 1.f / all : 0.f;
-    const int t = s.first + r / G, hq = h * G + r % G;
-    *(elem4 *)(a.O + t * a.out_stride_t + hq * a.out_stride_h + 4 * c) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-    if (c == 0) a.LSE[(int64_t)t * a.Hq + hq] = all > 0.f ? (top + fast_log2(all)) * kLn2 : -INFINITY;
-}
-
 template <int D, int RB, bool E8>
 static int launch_decode_t(const PagedFwdArgs &a, int max_rows, int workers, hipStream_t st)
 {
@@ -592,8 +461,8 @@ static int launch_decode_t(const PagedFwdArgs &a, int max_rows, int workers, hip
     } else {
         hipLaunchKernelGGL((attn_paged_decode_kernel<D, RB, E8, true>), dim3(workers), dim3(C::kThreads), C::kLds, st, a,
                            max_rows);
-        hipLaunchKernelGGL((attn_paged_merge_kernel<D, RB, E8>), dim3(a.b.B * a.Hkv, max_rows), dim3(256), 0, st, a,
-                           max_rows, workers);
+        hipLaunchKernelGGL((attn_paged_join_kernel<D, 1024 / D>), dim3(workers, max_rows), dim3(256), 0, st, a,
+                           PagedSlots<elem>(a.workspace, workers, 16 * RB, D), 16 * RB);
     }
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
