@@ -23,6 +23,7 @@ struct PagedAppendArgsT {
     void *K_cache, *V_cache;
     float *k_scale, *v_scale;  // NULL: 16-bit cache
     int Hq, Hkv, D, rot;
+    uint32_t nu_magic;  // ceil(2^32 / units of a row); one unit: 0
     int64_t q_stride_t, q_stride_h, out_stride_t, out_stride_h, kv_stride_t, kv_stride_h;
     int64_t cache_stride_p, cache_stride_h, cache_stride_s;
 };

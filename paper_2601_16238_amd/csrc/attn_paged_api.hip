@@ -20,7 +20,9 @@ int check_paged(const attn_paged_params_t *p, bool e4m3)
     if (p->page_size < 16 || p->page_size > 4096 || (p->page_size & (p->page_size - 1))) return ATTN_ERR_SHAPE;
     if (p->table_stride < p->table_width) return ATTN_ERR_STRIDE;
     if ((int64_t)p->table_width * p->page_size > lim || (int64_t)p->T * p->Hq > lim ||
-        p->T + 2 * (int64_t)p->B > lim || p->Hq > 65535)
+        p->Hq > 65535 ||
+        // (work-groups of the appending kernel)
+        ((int64_t)p->T / p->page_size + 2 * (int64_t)p->B) * p->Hkv * 2 + p->T > lim)
         return ATTN_ERR_SHAPE;
     for (int64_t s : {p->q_stride_t, p->q_stride_h, p->out_stride_t, p->out_stride_h})
         if (s < 0 || s % 8) return ATTN_ERR_STRIDE;

@@ -1,124 +1,263 @@
 // Appending rows to the paged key/value cache (include/attn_paged.h): K rotated on the way, Q beside it.
+//
+// Nothing is computed that would count: the kernels move bytes.  A row is worked on in units of twice W columns: columns
+// j .. j+W-1 and their partners j + rot/2 .., which are rotated together, or 2 W consecutive ones behind the rotated.
+// W = 8 (16-byte accesses) where such units cover a row, that is rot and D are multiples of 16, otherwise 4.
 #include "attn_paged.hpp"
 
 namespace attn {
 
-constexpr int kAppendThreads = 256;
 constexpr float kE4m3Max = 448.0f;
 
-// Column c of a row at position p, rotated: the same two fused multiply-adds as the rotary kernel's.
-__device__ __forceinline__ float rotated(const PagedAppendArgs &a, const elem *row, int c, int64_t p)
+template <int W>
+struct Unit {
+    float a[W], b[W];  // columns A .. and B ..
+};
+template <int W>
+struct Columns {
+    int A, B;
+    bool turned;
+    __device__ Columns(int u, int rot)
+    {
+        const int pairs = rot / (2 * W);
+        turned = u < pairs;
+        A = turned ? u * W : rot + (u - pairs) * 2 * W;
+        B = turned ? A + rot / 2 : A + W;
+    }
+};
+template <int W>
+__device__ __forceinline__ void load_columns(const elem *p, float (&x)[W])
 {
-    const int half = a.rot / 2;
-    const float x = (float)row[c];
-    if (c >= a.rot) return x;
-    const int j = c < half ? c : c - half;
-    const float cs = a.cos_table[p * half + j], sn = a.sin_table[p * half + j];
-    return c < half ? __builtin_fmaf(x, cs, -((float)row[c + half] * sn)) : __builtin_fmaf(x, cs, (float)row[j] * sn);
+    typedef elem vec __attribute__((ext_vector_type(W)));
+    const vec v = *(const vec *)p;
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = (float)v[i];
 }
-
-// One work-group for each token: its Q row, and with a 16-bit cache its K and V rows.
-__global__ void __launch_bounds__(kAppendThreads) attn_paged_append_kernel(const PagedAppendArgs a)
+template <int W>
+__device__ __forceinline__ void store_columns(elem *p, const float (&x)[W])
 {
-    const int t = blockIdx.x, b = paged_seq_of(a.b, t);
-    if (b == a.b.B) return;
-    const PagedSeq s = paged_seq(a.b, b);
-    const int p = s.len - s.n + t - s.first;
-    if (t < s.first || p < 0) return;
-    const int D = a.D;
-    if (a.Q_rot) {
-        for (int i = threadIdx.x; i < a.Hq * D / 2; i += kAppendThreads) {
-            // (both columns of a pair by one thread: Q_rot may be Q)
-            const int h = i / (D / 2), j = i - h * (D / 2), half = a.rot / 2;
-            const int c0 = j < half ? j : j + half, c1 = j < half ? j + half : j + D / 2;
-            const int lo = j < half ? c0 : 2 * j, hi = j < half ? c1 : 2 * j + 1;
-            const elem *row = a.Q + t * a.q_stride_t + h * a.q_stride_h;
-            const float y0 = rotated(a, row, lo, p), y1 = rotated(a, row, hi, p);
-            elem *out = a.Q_rot + t * a.out_stride_t + h * a.out_stride_h;
-            out[lo] = (elem)y0;
-            out[hi] = (elem)y1;
+    typedef elem vec __attribute__((ext_vector_type(W)));
+    typedef float vecf __attribute__((ext_vector_type(W)));
+    vecf v;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = x[i];
+    *(vec *)p = __builtin_convertvector(v, vec);
+}
+// Rotated by row p of the tables: the two fused multiply-adds of the rotary kernel, so that both give the same bits.
+template <int W>
+__device__ __forceinline__ void turn(const PagedAppendArgs &a, int64_t p, int j, Unit<W> &x)
+{
+    const float *cs = a.cos_table + p * (a.rot / 2) + j, *sn = a.sin_table + p * (a.rot / 2) + j;
+#pragma unroll
+    for (int q = 0; q < W; q += 4) {
+        const f32x4 c = *(const f32x4 *)(cs + q), s = *(const f32x4 *)(sn + q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = x.a[q + i], hi = x.b[q + i];
+            x.a[q + i] = __builtin_fmaf(lo, c[i], -(hi * s[i]));
+            x.b[q + i] = __builtin_fmaf(hi, c[i], lo * s[i]);
         }
     }
-    const int page = a.b.page_of(b, p);
-    if (a.k_scale || !a.b.is_page(page)) return;
-    for (int i = threadIdx.x; i < a.Hkv * D; i += kAppendThreads) {
-        const int h = i / D, c = i - h * D;
-        const int64_t from = t * a.kv_stride_t + h * a.kv_stride_h;
-        const int64_t to = page * a.cache_stride_p + h * a.cache_stride_h +
-                           (p & (a.b.page_size() - 1)) * a.cache_stride_s + c;
-        ((elem *)a.K_cache)[to] = (elem)rotated(a, a.K + from, c, p);
-        ((elem *)a.V_cache)[to] = a.V[from + c];
+}
+
+// i divided by the units of a row.
+__device__ __forceinline__ int row_of(const PagedAppendArgs &a, int i) { return a.nu_magic ? __umulhi(i, a.nu_magic) : i; }
+
+// The rows of token t by one work-group: of Q, and (KV) of K and V, with a 16-bit cache.
+template <int W, bool KV>
+__device__ __forceinline__ void append_token(const PagedAppendArgs &a, int t)
+{
+    const int b = paged_seq_of(a.b, t);
+    if (b == a.b.B) return;
+    const PagedSeq s = paged_seq_scalar(a.b, __builtin_amdgcn_readfirstlane(b));
+    const int p = s.len - s.n + t - s.first;
+    if (t < s.first || p < 0) return;
+    const int nu = a.D / (2 * W), Hq = a.Q_rot ? a.Hq : 0;
+    int page = -1;
+    if (KV) page = scalar_load(a.b.page_table + (int64_t)b * a.b.table_stride + (p >> a.b.page_shift));
+    const int rows = Hq + (KV && a.b.is_page(page) ? 2 * a.Hkv : 0);
+    const int64_t to = page * a.cache_stride_p + (p & (a.b.page_size() - 1)) * a.cache_stride_s;
+    for (int i = threadIdx.x; i < rows * nu; i += blockDim.x) {
+        const int row = row_of(a, i), u = i - row * nu;
+        const bool is_q = row < Hq, is_k = row < Hq + a.Hkv;
+        const int h = is_q ? row : is_k ? row - Hq : row - Hq - a.Hkv;
+        const Columns<W> c(u, is_k ? a.rot : 0);
+        const elem *from = is_q ? a.Q + t * a.q_stride_t + h * a.q_stride_h
+                                : (is_k ? a.K : a.V) + t * a.kv_stride_t + h * a.kv_stride_h;
+        elem *out = is_q ? a.Q_rot + t * a.out_stride_t + h * a.out_stride_h
+                         : (elem *)(is_k ? a.K_cache : a.V_cache) + to + h * a.cache_stride_h;
+        Unit<W> x;
+        load_columns<W>(from + c.A, x.a);
+        load_columns<W>(from + c.B, x.b);
+        if (c.turned) turn<W>(a, p, c.A, x);
+        store_columns<W>(out + c.A, x.a);
+        store_columns<W>(out + c.B, x.b);
     }
 }
 
-// The least power of two, 2^-100 at least, by which values of up to amax (> 0) fit e4m3: 448 = 1.75 * 2^8.
+template <int W>
+__global__ void __launch_bounds__(512) attn_paged_append_kernel(const PagedAppendArgs a)
+{
+    append_token<W, true>(a, blockIdx.x);
+}
+
+// The least power of two, 2^-100 at least, by which values of up to amax fit e4m3: 448 = 1.75 * 2^8.
 __device__ __forceinline__ float e4m3_scale(float amax)
 {
     const uint32_t u = __float_as_uint(amax);
     const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
     return __uint_as_float((uint32_t)(min(max(e, -100), 120) + 127) << 23);
 }
-__device__ __forceinline__ uint8_t to_e4m3(float x)
+__device__ __forceinline__ uint32_t to_e4m3(float x0, float x1, float x2, float x3)
 {
-    x = fminf(fmaxf(x, -kE4m3Max), kE4m3Max);
-    return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false);
+    auto in = [](float x) { return fminf(fmaxf(x, -kE4m3Max), kE4m3Max); };
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(in(x0), in(x1), 0, false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(in(x2), in(x3), lo, true);
+}
+template <int W>
+__device__ __forceinline__ void store_codes(uint8_t *p, const float (&x)[W], float by)
+{
+#pragma unroll
+    for (int i = 0; i < W; i += 4)
+        *(uint32_t *)(p + i) = to_e4m3(x[i] * by, x[i + 1] * by, x[i + 2] * by, x[i + 3] * by);
 }
 
-// e4m3 cache: one work-group for each page that gets rows (slot), head and tensor.  Sequence b has the slots from
-// q_start[b] / P + 2 b on: n rows touch at most n / P + 2 pages, so they do not reach into the next one's.
-__global__ void __launch_bounds__(kAppendThreads) attn_paged_append8_kernel(const PagedAppendArgs a)
+// e4m3 cache: one work-group for each page that gets rows (slot), head and tensor; behind them one for each token's Q.
+// Sequence b has the slots from q_start[b] / P + 2 b on: n rows touch at most n / P + 2 pages, so they do not reach into
+// the next one's.  A page's new values are read once, where a thread can keep its units of them (kKeep), and a second
+// time for pages of more than kKeep THREADS units.
+template <int W, int THREADS>
+__global__ void __launch_bounds__(THREADS) attn_paged_append8_kernel(const PagedAppendArgs a, const int slots)
 {
-    __shared__ float most[kAppendThreads];
-    const int P = a.b.page_size(), sh = a.b.page_shift, u = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, D = a.D;
-    int b = 0;
-    while (b < a.b.B && (min(max(a.b.q_start[b + 1], 0), a.b.T) >> sh) + 2 * (b + 1) <= u) ++b;
-    if (b == a.b.B) return;
-    const PagedSeq s = paged_seq(a.b, b);
-    const int older = max(s.len - s.n, 0), slot = u - (s.first >> sh) - 2 * b;
-    if (slot < 0) return;
-    const int in_seq = (older >> sh) + slot;  // which of the sequence's pages
+    constexpr int kKeep = 4, kWaves = THREADS / 64;
+    __shared__ float most[kWaves];
+    const int tid = threadIdx.x, l = tid & 63;
+    if ((int)blockIdx.x >= slots * a.Hkv * 2) {
+        append_token<W, false>(a, blockIdx.x - slots * a.Hkv * 2);
+        return;
+    }
+    const int z = blockIdx.x & 1, h = (blockIdx.x >> 1) % a.Hkv, slot = (blockIdx.x >> 1) / a.Hkv;
+    const int P = a.b.page_size(), sh = a.b.page_shift, D = a.D;
+    int b = -1;
+    for (int b0 = 0; b0 < a.b.B && b < 0; b0 += 64) {
+        const int i = b0 + l;
+        const int end = (min(max(a.b.q_start[min(i, a.b.B - 1) + 1], 0), a.b.T) >> sh) + 2 * (i + 1);
+        const uint64_t behind = __builtin_amdgcn_ballot_w64(i < a.b.B && end > slot);
+        if (behind) b = b0 + __builtin_ctzll(behind);
+    }
+    if (b < 0) return;
+    const PagedSeq s = paged_seq_scalar(a.b, __builtin_amdgcn_readfirstlane(b));
+    const int older = max(s.len - s.n, 0), nth = slot - (s.first >> sh) - 2 * b;
+    if (nth < 0) return;
+    const int in_seq = (older >> sh) + nth;  // which of the sequence's pages
     if (s.n == 0 || ((int64_t)in_seq << sh) >= s.len) return;
-    const int page = a.b.page_of(b, in_seq << sh);
+    const int page = scalar_load(a.b.page_table + (int64_t)b * a.b.table_stride + in_seq);
     if (!a.b.is_page(page)) return;
     const int p0 = in_seq << sh, lo = max(older, p0), hi = min(s.len, p0 + P);
-    const elem *from = (blockIdx.z ? a.V : a.K) + h * a.kv_stride_h;
-    uint8_t *to = (uint8_t *)(blockIdx.z ? a.V_cache : a.K_cache) + page * a.cache_stride_p + h * a.cache_stride_h;
-    float *scale = (blockIdx.z ? a.v_scale : a.k_scale) + (int64_t)page * a.Hkv + h;
+    const int rot = z ? 0 : a.rot, nu = D / (2 * W), units = (hi - lo) * nu;
+    const elem *from = (z ? a.V : a.K) + h * a.kv_stride_h;
+    uint8_t *to = (uint8_t *)(z ? a.V_cache : a.K_cache) + page * a.cache_stride_p + h * a.cache_stride_h;
+    float *scale = (z ? a.v_scale : a.k_scale) + (int64_t)page * a.Hkv + h;
     const int t0 = s.first + s.n - s.len;  // packed row of position 0
-    auto value = [&](int i) {
-        const int p = lo + i / D, c = i % D;
-        const elem *row = from + (t0 + p) * a.kv_stride_t;
-        return blockIdx.z ? (float)row[c] : rotated(a, row, c, p);
+    // which unit: row and columns
+    auto unit = [&](int i, Unit<W> &x) __attribute__((always_inline)) {
+        const int row = row_of(a, i), p = lo + row;
+        const Columns<W> c(i - row * nu, rot);
+        const elem *src = from + (t0 + p) * a.kv_stride_t;
+        load_columns<W>(src + c.A, x.a);
+        load_columns<W>(src + c.B, x.b);
+        if (c.turned) turn<W>(a, p, c.A, x);
     };
+    auto largest = [&](const Unit<W> &x, float most_) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) most_ = fmaxf(most_, fmaxf(fabsf(x.a[i]), fabsf(x.b[i])));
+        return most_;
+    };
+    auto store = [&](int i, const Unit<W> &x, float by) __attribute__((always_inline)) {
+        const int row = row_of(a, i);
+        const Columns<W> c(i - row * nu, rot);
+        uint8_t *out = to + (lo - p0 + row) * a.cache_stride_s;
+        store_codes<W>(out + c.A, x.a, by);
+        store_codes<W>(out + c.B, x.b, by);
+    };
+    Unit<W> kept[kKeep];
     float amax = 0.f;
-    for (int i = tid; i < (hi - lo) * D; i += kAppendThreads) amax = fmaxf(amax, fabsf(value(i)));
-    most[tid] = amax;
-    __syncthreads();
-    for (int n = kAppendThreads / 2; n; n /= 2) {
-        if (tid < n) most[tid] = fmaxf(most[tid], most[tid + n]);
+#pragma unroll
+    for (int k = 0; k < kKeep; ++k) {
+        const int i = tid + k * THREADS;
+        if (i < units) {
+            unit(i, kept[k]);
+            amax = largest(kept[k], amax);
+        }
+    }
+    for (int i = tid + kKeep * THREADS; i < units; i += THREADS) {
+        Unit<W> x;
+        unit(i, x);
+        amax = largest(x, amax);
+    }
+#pragma unroll
+    for (int d = 32; d; d /= 2) amax = fmaxf(amax, __shfl_xor(amax, d));
+    if constexpr (kWaves > 1) {
+        if (l == 0) most[tid >> 6] = amax;
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) amax = fmaxf(amax, most[i]);
     }
     const float before = lo > p0 ? *scale : 0.f;
-    const float by = fmaxf(e4m3_scale(most[0]), before);
-    if (by > before)
-        for (int i = tid; i < (lo - p0) * D; i += kAppendThreads) {
-            uint8_t *x = to + i / D * a.cache_stride_s + i % D;
-            *x = to_e4m3(__builtin_amdgcn_cvt_f32_fp8(*x, 0) * (before / by));
+    const float now = fmaxf(e4m3_scale(amax), before), by = 1.0f / now;
+    // the older keys take the larger scale
+    if (now > before && lo > p0) {
+        const float ratio = before / now;
+        for (int i = tid; i < (lo - p0) * (D / 16); i += THREADS) {
+            const int row = i / (D / 16);
+            u32x4 *at = (u32x4 *)(to + row * a.cache_stride_s + (i - row * (D / 16)) * 16), v = *at;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(v[k], false), y = __builtin_amdgcn_cvt_pk_f32_fp8(v[k], true);
+                v[k] = to_e4m3(x[0] * ratio, x[1] * ratio, y[0] * ratio, y[1] * ratio);
+            }
+            *at = v;
         }
-    for (int i = tid; i < (hi - lo) * D; i += kAppendThreads)
-        to[(lo - p0 + i / D) * a.cache_stride_s + i % D] = to_e4m3(value(i) / by);
-    __syncthreads();
-    if (tid == 0) *scale = by;
+    }
+#pragma unroll
+    for (int k = 0; k < kKeep; ++k) {
+        const int i = tid + k * THREADS;
+        if (i < units) store(i, kept[k], by);
+    }
+    for (int i = tid + kKeep * THREADS; i < units; i += THREADS) {
+        Unit<W> x;
+        unit(i, x);
+        store(i, x, by);
+    }
+    // (every wave has read the old one)
+    if constexpr (kWaves > 1) __syncthreads();
+    if (tid == 0) *scale = now;
+}
+
+template <int W>
+static int launch_append_w(PagedAppendArgs a, hipStream_t st)
+{
+    const int nu = a.D / (2 * W);
+    a.nu_magic = (uint32_t)((((uint64_t)1 << 32) + nu - 1) / nu);
+    if (!a.k_scale) {
+        const int units = ((a.Q_rot ? a.Hq : 0) + 2 * a.Hkv) * nu;
+        hipLaunchKernelGGL(attn_paged_append_kernel<W>, dim3(a.b.T), dim3(units >= 512 ? 512 : (units + 63) / 64 * 64), 0, st,
+                           a);
+    } else {
+        const int slots = (a.b.T >> a.b.page_shift) + 2 * a.b.B;
+        const dim3 grid((unsigned)(slots * a.Hkv * 2 + (a.Q_rot ? a.b.T : 0)));
+        // few new rows a sequence: a wave for each page and head, otherwise four
+        if (a.b.T <= 4 * (int64_t)a.b.B)
+            hipLaunchKernelGGL((attn_paged_append8_kernel<W, 64>), grid, dim3(64), 0, st, a, slots);
+        else
+            hipLaunchKernelGGL((attn_paged_append8_kernel<W, 256>), grid, dim3(256), 0, st, a, slots);
+    }
+    return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 int launch_paged_append(const PagedAppendArgs &a, hipStream_t st)
 {
-    if (a.Q_rot || !a.k_scale)
-        hipLaunchKernelGGL(attn_paged_append_kernel, dim3(a.b.T), dim3(kAppendThreads), 0, st, a);
-    if (a.k_scale)
-        hipLaunchKernelGGL(attn_paged_append8_kernel, dim3((a.b.T >> a.b.page_shift) + 2 * a.b.B, a.Hkv, 2),
-                           dim3(kAppendThreads), 0, st, a);
-    return hipGetLastError() == hipSuccess ? 0 : -1;
+    return a.rot % 16 == 0 && a.D % 16 == 0 ? launch_append_w<8>(a, st) : launch_append_w<4>(a, st);
 }
 
 }  // namespace attn
