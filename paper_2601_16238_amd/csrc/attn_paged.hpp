@@ -52,8 +52,8 @@ int launch_paged_fwd(const PagedFwdArgsT<_Float16> &a, hipStream_t st);
 int launch_paged_decode(const PagedFwdArgsT<__bf16> &a, int D, int max_rows, int workers, hipStream_t st);
 int launch_paged_decode(const PagedFwdArgsT<_Float16> &a, int D, int max_rows, int workers, hipStream_t st);
 
-int launch_paged_chunk(const PagedFwdArgsT<__bf16> &a, int D, int longer, int workers, void *workspace, hipStream_t st);
-int launch_paged_chunk(const PagedFwdArgsT<_Float16> &a, int D, int longer, int workers, void *workspace, hipStream_t st);
+int launch_paged_chunk(const PagedFwdArgsT<__bf16> &a, int D, int workers, hipStream_t st);
+int launch_paged_chunk(const PagedFwdArgsT<_Float16> &a, int D, int workers, hipStream_t st);
 
 // Work in spans: a work-group takes the same number of tiles of keys as every other, from wherever its span begins to
 // wherever it ends.  Of a unit of rows that several have worked on, each leaves a partial result in the workspace: the
@@ -71,6 +71,7 @@ __host__ __device__ constexpr int64_t paged_span_bytes(int64_t workers, int rows
 {
     return (paged_slots_bytes(workers, rows, D) + workers * (int64_t)sizeof(PagedJoin) + 255) / 256 * 256;
 }
+constexpr float kJoinMinusHuge = -1.0e30f;  // what a maximum starts from
 template <typename E>
 struct PagedSlots {
     float *part, *m, *l;
@@ -80,14 +81,13 @@ struct PagedSlots {
           join((PagedJoin *)(l + 2 * workers * rows)) {}
 };
 
-// Which kernels a call takes, by what the host knows of the batch: the decoding kernel for the sequences of up to
-// decode_rows rows (new tokens times the query heads of a K/V head; 0: it is not launched), the other for longer ones.
+// Which kernel a call takes, by what the host knows of the batch.
 struct PagedPlan {
     int kernel_d;     // 64, 128 or 256
-    int decode_rows, decode_workers;  // workers 0: one work-group for each unit of rows
-    bool chunks;
-    int chunk_workers;
-    size_t decode_bytes, bytes;       // workspace: the decoding kernel's part, all
+    int decode_rows;  // the decoding kernel, for sequences of up to so many rows (new tokens times the query heads of a
+                      // K/V head); 0: the kernel of many rows
+    int workers;      // 0: one work-group for each unit of rows
+    size_t bytes;     // workspace
 };
 constexpr int kDecodeSpan = 4, kChunkSpan = 4;  // tiles of a span, at least
 PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3);
@@ -140,52 +140,6 @@ __device__ __forceinline__ int block_scan(int v, int *lds, int &all)
     return v;
 }
 
-// The span of worker w of `workers`: `tiles(b)` are those of sequence b with one head, of which there are `heads`.
-// Where the span begins: sequence b, and how many tiles lie in front of that sequence (all heads).
-struct PagedSpan {
-    int64_t begin, front, size;
-    int left, b;  // tiles of the span (0: none)
-};
-template <int NW, typename Tiles>
-__device__ __forceinline__ PagedSpan paged_span(int B, int heads, int w, int workers, int least, int *lds, Tiles tiles)
-{
-    const int tid = threadIdx.x;
-    int64_t total = 0;
-    int mine = 0, sum = 0, all = 0;
-    for (int b0 = 0; b0 < B; b0 += NW * 64) {
-        mine = b0 + tid < B ? tiles(b0 + tid) : 0;
-        sum = block_scan<NW>(mine, lds, all);
-        total += all;
-    }
-    PagedSpan s = {};
-    total *= heads;
-    s.size = max((int64_t)least, (total + workers - 1) / workers);
-    s.begin = w * s.size;
-    const int64_t left = min(s.size, total - s.begin);
-    s.left = __builtin_amdgcn_readfirstlane((int)max(left, (int64_t)0));
-    if (s.left == 0) return s;
-    // (one round: its sums are still there)
-    for (int b0 = 0; b0 < B; b0 += NW * 64) {
-        if (B > NW * 64) {
-            mine = b0 + tid < B ? tiles(b0 + tid) : 0;
-            sum = block_scan<NW>(mine, lds, all);
-        }
-        if ((s.front + all) * heads > s.begin) {
-            __syncthreads();
-            if ((s.front + sum) * heads > s.begin && (s.front + sum - mine) * heads <= s.begin) {
-                lds[0] = b0 + tid;
-                lds[1] = sum - mine;
-            }
-            __syncthreads();
-            s.b = __builtin_amdgcn_readfirstlane(lds[0]);
-            s.front = (s.front + __builtin_amdgcn_readfirstlane(lds[1])) * heads;
-            return s;
-        }
-        s.front += all;
-    }
-    return s;
-}
-
 // A value of device memory that no kernel writes while this one runs, by a scalar load.
 template <typename T>
 __device__ __forceinline__ T scalar_load(const T *p)
@@ -198,6 +152,80 @@ __device__ __forceinline__ PagedSeq paged_seq_scalar(const PagedBatch &a, int b)
     s.first = min(max(scalar_load(a.q_start + b), 0), a.T);
     s.n = max(min(scalar_load(a.q_start + b + 1), a.T) - s.first, 0);
     s.len = min(max(scalar_load(a.kv_lens + b), 0), a.table_width << a.page_shift);
+    return s;
+}
+
+// The span of worker w of `workers`: `tiles(seq)` are those of a sequence with one head, of which there are `heads`.
+// Where the span begins: sequence b, and how many tiles lie in front of that sequence (all heads).
+struct PagedSpan {
+    int64_t begin, front, size;
+    int left, b;  // tiles of the span (0: none)
+    PagedSeq seq;
+};
+__device__ __forceinline__ int64_t div_up(int64_t x, int y)
+{
+    // (a division of 64 bits takes four times as long)
+    return x < (1 << 30) ? (int64_t)(((unsigned)x + y - 1) / (unsigned)y) : (x + y - 1) / y;
+}
+template <int NW, typename Tiles>
+__device__ __forceinline__ PagedSpan paged_span(const PagedBatch &a, int heads, int w, int workers, int least, int *lds,
+                                                Tiles tiles)
+{
+    const int tid = threadIdx.x, l = tid & 63, B = a.B;
+    PagedSpan s = {};
+    auto cut = [&](int64_t total) __attribute__((always_inline)) {
+        s.size = max((int64_t)least, div_up(total, workers));
+        s.begin = w * s.size;
+        s.left = __builtin_amdgcn_readfirstlane((int)max(min(s.size, total - s.begin), (int64_t)0));
+    };
+    if (B <= 64) {
+        // every wave by itself: without barriers, and with what it has loaded
+        const PagedSeq q = paged_seq(a, min(l, B - 1));
+        const int mine = l < B ? tiles(q) : 0;
+        int sum = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_up(sum, d);
+            if (l >= d) sum += x;
+        }
+        cut((int64_t)__builtin_amdgcn_readlane(sum, 63) * heads);
+        if (s.left == 0) return s;
+        s.b = __builtin_ctzll(__builtin_amdgcn_ballot_w64((int64_t)sum * heads > s.begin));
+        s.front = (int64_t)__builtin_amdgcn_readlane(sum - mine, s.b) * heads;
+        s.seq.first = __builtin_amdgcn_readlane(q.first, s.b);
+        s.seq.n = __builtin_amdgcn_readlane(q.n, s.b);
+        s.seq.len = __builtin_amdgcn_readlane(q.len, s.b);
+        return s;
+    }
+    int64_t total = 0;
+    int mine = 0, sum = 0, all = 0;
+    for (int b0 = 0; b0 < B; b0 += NW * 64) {
+        mine = b0 + tid < B ? tiles(paged_seq(a, b0 + tid)) : 0;
+        sum = block_scan<NW>(mine, lds, all);
+        total += all;
+    }
+    cut(total * heads);
+    if (s.left == 0) return s;
+    // (one round: its sums are still there)
+    for (int b0 = 0; b0 < B; b0 += NW * 64) {
+        if (B > NW * 64) {
+            mine = b0 + tid < B ? tiles(paged_seq(a, b0 + tid)) : 0;
+            sum = block_scan<NW>(mine, lds, all);
+        }
+        if ((s.front + all) * heads > s.begin) {
+            __syncthreads();
+            if ((s.front + sum) * heads > s.begin && (s.front + sum - mine) * heads <= s.begin) {
+                lds[0] = b0 + tid;
+                lds[1] = sum - mine;
+            }
+            __syncthreads();
+            s.b = __builtin_amdgcn_readfirstlane(lds[0]);
+            s.front = (s.front + __builtin_amdgcn_readfirstlane(lds[1])) * heads;
+            s.seq = paged_seq_scalar(a, s.b);
+            return s;
+        }
+        s.front += all;
+    }
     return s;
 }
 
@@ -224,27 +252,53 @@ __device__ __forceinline__ float scale_rest(float scale)
     return u ? __uint_as_float((u & 0x7fffffu) | 0x3f800000u) : 0.f;
 }
 
-// The partial results of the units that worker blockIdx.x has the first tile of, joined: PAR groups of threads share the
-// pieces of a row, the other threads of the work-group take further rows (grid y).
+// The partial results of the units that worker blockIdx.x has the first tile of, joined.  A work-group has kRows rows (grid
+// y), 256 / kRows threads each: D / 4 columns of four, and PAR groups of them that share the pieces.  64 pieces at a
+// time: their maxima and sums come through LDS, so that no load waits for another but the record's.
 template <int D, int PAR>
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedFwdArgs a, const PagedSlots<elem> s, const int R)
 {
-    constexpr int kCols = D / 4, kRows = 256 / kCols / PAR;
+    constexpr int kCols = D / 4, kRows = 256 / kCols / PAR, kPieces = 64;
+    __shared__ float ms[kPieces][kRows], ls[kPieces][kRows];
     __shared__ f32x4 sum[PAR > 1 ? PAR : 1][PAR > 1 ? kCols : 1];
     static_assert(PAR == 1 || kRows == 1, "one row, or one thread for all pieces");
     const PagedJoin j = s.join[blockIdx.x];
-    const int tid = threadIdx.x, c = tid % kCols, p = PAR > 1 ? tid / kCols : 0;
-    const int r = blockIdx.y * kRows + (PAR > 1 ? 0 : tid / kCols);
-    if (j.pieces == 0 || (PAR > 1 ? r : (int)blockIdx.y * kRows) >= j.rows) return;
-    auto at = [&](int i) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0)) * R + r; };
+    const int tid = threadIdx.x, c = tid % kCols, p = PAR > 1 ? tid / kCols : 0, rr = PAR > 1 ? 0 : tid / kCols;
+    const int r0 = blockIdx.y * kRows, r = r0 + rr;
+    if (j.pieces == 0 || r0 >= j.rows) return;
+    auto at = [&](int i, int row) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0)) * R + row; };
+    const bool mine = r < j.rows && 4 * c < a.Dr;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float top = -INFINITY, all = 0.f;
-    if (r < j.rows) {
-        for (int i = 0; i < j.pieces; ++i) top = fmaxf(top, s.m[at(i)]);
-        for (int i = 0; i < j.pieces; ++i) all += s.l[at(i)] * fast_exp2(s.m[at(i)] - top);
-        if (4 * c < a.Dr)
-            for (int i = p; i < j.pieces; i += PAR)
-                x += *(const f32x4 *)(s.part + at(i) * D + 4 * c) * fast_exp2(s.m[at(i)] - top);
+    float top = kJoinMinusHuge, all = 0.f;
+    for (int i0 = 0; i0 < j.pieces; i0 += kPieces) {
+        const int n = min(j.pieces - i0, kPieces);
+        if (i0) __syncthreads();
+        for (int k = tid; k < n * kRows; k += 256) {
+            const int i = k / kRows, row = k % kRows;
+            const bool is = r0 + row < j.rows;
+            ms[i][row] = is ? s.m[at(i0 + i, r0 + row)] : 0.f;
+            ls[i][row] = is ? s.l[at(i0 + i, r0 + row)] : 0.f;
+        }
+        __syncthreads();
+        float to = top;
+        for (int i = 0; i < n; ++i) to = fmaxf(to, ms[i][rr]);
+        const float keep = fast_exp2(top - to);
+        x *= keep;
+        all *= keep;
+        top = to;
+        for (int i = 0; i < n; ++i) all += ls[i][rr] * fast_exp2(ms[i][rr] - to);
+        if (mine) {
+            const float *part = s.part + at(i0 + p, r) * D + 4 * c;
+            const int64_t step = 2 * (int64_t)PAR * R * D;
+            int i = p;
+            if (i0 == 0 && i == 0) {  // (the first piece lies in its worker's other slot)
+                x += *(const f32x4 *)part * fast_exp2(ms[0][rr] - to);
+                part = s.part + at(PAR, r) * D + 4 * c;
+                i = PAR;
+            }
+#pragma unroll 4
+            for (; i < n; i += PAR, part += step) x += *(const f32x4 *)part * fast_exp2(ms[i][rr] - to);
+        }
     }
     if constexpr (PAR > 1) {
         sum[p][c] = x;
@@ -253,7 +307,7 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedFwdArgs
 #pragma unroll
         for (int i = 1; i < PAR; ++i) x += sum[i][c];
     }
-    if (r >= j.rows || 4 * c >= a.Dr) return;
+    if (!mine) return;
     const float inv = all > 0.f ? 1.f / all : 0.f;
     const int G = a.Hq / a.Hkv, row = j.row0 + r, t = j.first + row / G, hq = j.head * G + row % G;
     *(elem4 *)(a.O + t * a.out_stride_t + hq * a.out_stride_h + 4 * c) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);

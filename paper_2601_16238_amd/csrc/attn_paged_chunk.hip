@@ -34,14 +34,9 @@ struct ChunkCfg {
 };
 
 // Units of rows of a sequence: rt has the rows rt BR .. of the sequence's n G.
-struct ChunkSeq {
-    PagedSeq s;
-    int row_tiles;
-};
-__device__ __forceinline__ ChunkSeq chunk_seq(const PagedSeq &s, int G, int longer, int max_q, int BR)
+__device__ __forceinline__ int chunk_row_tiles(const PagedSeq &s, int G, int max_q, int BR)
 {
-    const int64_t rows = (int64_t)s.n * G;
-    return {s, rows <= longer || s.n > max_q ? 0 : (int)((rows + BR - 1) / BR)};
+    return s.n > max_q ? 0 : (int)(((unsigned)(s.n * G) + BR - 1) / BR);
 }
 // Tiles of keys that the rows up to the end of new token `token` see (none: one, in which nothing is seen).
 __device__ __forceinline__ int chunk_tiles(const PagedSeq &s, bool causal, int token)
@@ -63,12 +58,12 @@ struct ChunkWalk {
         return left ? token + 1 : token;
     }
 };
-__device__ __forceinline__ int chunk_cost(const PagedSeq &s, int G, int longer, int max_q, int BR, bool causal)
+__device__ __forceinline__ int chunk_cost(const PagedSeq &s, int G, int max_q, int BR, bool causal)
 {
-    const ChunkSeq c = chunk_seq(s, G, longer, max_q, BR);
+    const int row_tiles = chunk_row_tiles(s, G, max_q, BR);
     ChunkWalk walk(G, BR);
     int sum = 0;
-    for (int rt = 0; rt < c.row_tiles; ++rt) sum += chunk_tiles(s, causal, walk.next());
+    for (int rt = 0; rt < row_tiles; ++rt) sum += chunk_tiles(s, causal, walk.next());
     return sum;
 }
 
@@ -78,7 +73,7 @@ constexpr float kChunkMinusHuge = -1.0e30f;
 template <int D, bool E8, bool SPLIT>
 __global__ void __launch_bounds__((ChunkCfg<D, E8>::kThreads))
     __attribute__((amdgpu_waves_per_eu(ChunkCfg<D, E8>::kWaves, ChunkCfg<D, E8>::kWaves)))
-attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots, const int longer)
+attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
 {
     using C = ChunkCfg<D, E8>;
     using L = typename C::L;
@@ -99,19 +94,18 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots, cons
     ChunkWalk walk(G, BR);
     PagedSpan span = {};
     const int me = SPLIT ? xcd_contiguous_order(blockIdx.x, gridDim.x) : blockIdx.x;
-    auto load_seq = [&](int b) __attribute__((always_inline)) {
-        const ChunkSeq c = chunk_seq(paged_seq_scalar(a.b, b), G, longer, a.max_q, BR);
-        s = c.s;
-        row_tiles = c.row_tiles;
+    auto set_seq = [&](const PagedSeq &q) __attribute__((always_inline)) {
+        s = q;
+        row_tiles = chunk_row_tiles(q, G, a.max_q, BR);
     };
     if constexpr (SPLIT) {
-        span = paged_span<NW>(B, Hkv, me, gridDim.x, kChunkSpan, scan,
-                              [&](int b) { return chunk_cost(paged_seq(a.b, b), G, longer, a.max_q, BR, causal); });
+        span = paged_span<NW>(a.b, Hkv, me, gridDim.x, kChunkSpan, scan,
+                              [&](const PagedSeq &q) { return chunk_cost(q, G, a.max_q, BR, causal); });
         todo = span.left;
         if (tid == 0) slots.join[me].pieces = 0;
         if (todo == 0) return;
         u.b = span.b;
-        load_seq(u.b);
+        set_seq(span.seq);
         // which head, which unit of it and which of its tiles
         int cost = 0;
         for (int rt = 0; rt < row_tiles; ++rt) cost += chunk_tiles(s, causal, walk.next());
@@ -135,13 +129,14 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots, cons
         int b = -1;
         for (int b0 = 0; b0 < B && b < 0; b0 += 64) {
             const int bl = min(b0 + l, B - 1);
-            const ChunkSeq c = chunk_seq(paged_seq(a.b, bl), G, longer, a.max_q, BR);
-            const int64_t from = (int64_t)c.s.first * G / BR + bl;
-            const uint64_t is = __builtin_amdgcn_ballot_w64(b0 + l < B && slot >= from && slot < from + c.row_tiles);
+            const PagedSeq q = paged_seq(a.b, bl);
+            const int64_t from = (int64_t)q.first * G / BR + bl;
+            const uint64_t is = __builtin_amdgcn_ballot_w64(b0 + l < B && slot >= from &&
+                                                            slot < from + chunk_row_tiles(q, G, a.max_q, BR));
             if (is) b = __builtin_amdgcn_readfirstlane(b0 + __builtin_ctzll(is));
         }
         if (b < 0) return;
-        load_seq(b);
+        set_seq(paged_seq_scalar(a.b, b));
         u.rt = __builtin_amdgcn_readfirstlane((int)(slot - ((int64_t)s.first * G / BR + b)));
         u.b = b;
         for (int rt = 0; rt <= u.rt; ++rt) u.token = walk.next();
@@ -416,7 +411,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots, cons
             walk = ChunkWalk(G, BR);
             if (++u.h == Hkv) {
                 u.h = 0;
-                do load_seq(++u.b); while (row_tiles == 0);
+                do set_seq(paged_seq_scalar(a.b, ++u.b)); while (row_tiles == 0);
             }
         }
         u.token = walk.next();
@@ -425,35 +420,34 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots, cons
 }
 
 template <int D, bool E8>
-static int launch_chunk_t(const PagedFwdArgs &a, int longer, int workers, void *workspace, hipStream_t st)
+static int launch_chunk_t(const PagedFwdArgs &a, int workers, hipStream_t st)
 {
     using C = ChunkCfg<D, E8>;
     const void *kernel = workers ? (const void *)attn_paged_chunk_kernel<D, E8, true>
                                  : (const void *)attn_paged_chunk_kernel<D, E8, false>;
     if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds) != hipSuccess) return -1;
-    const PagedSlots<elem> slots(workspace, workers, C::kBR, D);
+    const PagedSlots<elem> slots(a.workspace, workers, C::kBR, D);
     if (!workers) {
         const int64_t units = (int64_t)a.b.T * (a.Hq / a.Hkv) / C::kBR + a.b.B;
         hipLaunchKernelGGL((attn_paged_chunk_kernel<D, E8, false>), dim3((unsigned)(units * a.Hkv)), dim3(C::kThreads),
-                           C::kLds, st, a, slots, longer);
+                           C::kLds, st, a, slots);
     } else {
-        hipLaunchKernelGGL((attn_paged_chunk_kernel<D, E8, true>), dim3(workers), dim3(C::kThreads), C::kLds, st, a, slots,
-                           longer);
+        hipLaunchKernelGGL((attn_paged_chunk_kernel<D, E8, true>), dim3(workers), dim3(C::kThreads), C::kLds, st, a, slots);
         hipLaunchKernelGGL((attn_paged_join_kernel<D, 1>), dim3(workers, C::kBR * D / 1024), dim3(256), 0, st, a, slots,
                            C::kBR);
     }
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-int launch_paged_chunk(const PagedFwdArgs &a, int D, int longer, int workers, void *workspace, hipStream_t st)
+int launch_paged_chunk(const PagedFwdArgs &a, int D, int workers, hipStream_t st)
 {
     if (a.k_scale)
-        return D == 64 ? launch_chunk_t<64, true>(a, longer, workers, workspace, st)
-             : D == 128 ? launch_chunk_t<128, true>(a, longer, workers, workspace, st)
-                        : launch_chunk_t<256, true>(a, longer, workers, workspace, st);
-    return D == 64 ? launch_chunk_t<64, false>(a, longer, workers, workspace, st)
-         : D == 128 ? launch_chunk_t<128, false>(a, longer, workers, workspace, st)
-                    : launch_chunk_t<256, false>(a, longer, workers, workspace, st);
+        return D == 64 ? launch_chunk_t<64, true>(a, workers, st)
+             : D == 128 ? launch_chunk_t<128, true>(a, workers, st)
+                        : launch_chunk_t<256, true>(a, workers, st);
+    return D == 64 ? launch_chunk_t<64, false>(a, workers, st)
+         : D == 128 ? launch_chunk_t<128, false>(a, workers, st)
+                    : launch_chunk_t<256, false>(a, workers, st);
 }
 
 }  // namespace attn

@@ -89,8 +89,7 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
 
     // ---- where the span begins
     struct Unit { int b, h, t, tiles, first, n, len; };  // sequence, K/V head, tile
-    auto load_seq = [&](Unit &u) __attribute__((always_inline)) {
-        const PagedSeq s = paged_seq_scalar(a.b, u.b);
+    auto set_seq = [&](Unit &u, const PagedSeq &s) __attribute__((always_inline)) {
         u.first = s.first;
         u.n = s.n;
         u.len = s.len;
@@ -100,13 +99,13 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
     int todo;  // tiles of the span that are not computed yet
     PagedSpan span = {};
     if constexpr (SPLIT) {
-        span = paged_span<NW>(B, Hkv, blockIdx.x, gridDim.x, kDecodeSpan, scan,
-                              [&](int b) { return decode_tiles(paged_seq(a.b, b), G, max_rows, TK); });
+        span = paged_span<NW>(a.b, Hkv, blockIdx.x, gridDim.x, kDecodeSpan, scan,
+                              [&](const PagedSeq &s) { return decode_tiles(s, G, max_rows, TK); });
         todo = span.left;
         if (tid == 0) slots.join[blockIdx.x].pieces = 0;
         if (todo == 0) return;
         nx.b = span.b;
-        load_seq(nx);
+        set_seq(nx, span.seq);
         const int in = __builtin_amdgcn_readfirstlane((int)(span.begin - span.front));
         nx.h = in / nx.tiles;
         nx.t = in - nx.h * nx.tiles;
@@ -114,7 +113,7 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         nx.b = blockIdx.x / Hkv;
         nx.h = blockIdx.x % Hkv;
         nx.t = 0;
-        load_seq(nx);
+        set_seq(nx, paged_seq_scalar(a.b, nx.b));
         todo = nx.tiles;
         if (todo == 0) return;
     }
@@ -140,14 +139,6 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
             v_at[j] = C::kPieces * 1024 + C::at(4 * g + (m16 >> 2), 2 * j + ((l >> 1) & 1)) + (l & 1) * 8;
         }
     }
-    // the lane's rows (as columns of S^T): query head and new token
-    int row_q[RB], row_h[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        row_q[rb] = (16 * rb + m16) / G;
-        row_h[rb] = 16 * rb + m16 - row_q[rb] * G;
-    }
-
     // ---- transfers
     struct Pages { int id[2]; };           // of the wave's two half blocks of a tile
     struct Scales { float k[2], v[2]; };
@@ -189,19 +180,30 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         }
     };
 
+    Pages nx_pages = pages_of(nx);
+    Scales sc = {};
+    issue(nx, nx_pages, 0, sc);
+
+    // the lane's rows (as columns of S^T): query head and new token
+    int row_q[RB], row_h[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        row_q[rb] = (16 * rb + m16) / G;
+        row_h[rb] = 16 * rb + m16 - row_q[rb] * G;
+    }
+
     // ---- a sequence's and head's state
     frag q[RB][C::kSteps];
+    // (the next unit's, requested with its first keys: where there are registers for them)
+    constexpr bool kAhead = RB == 1;
+    frag next_q[kAhead ? RB : 1][C::kSteps];
     f32x4 o[RB][C::kDB];
     float m[RB], lsum[RB];
     constexpr float kMinusHuge = -1.0e30f;
     constexpr float kSlack = 8.f;  // probabilities up to 2^8 before the reference maximum moves
-    auto begin_unit = [&](const Unit &u) __attribute__((always_inline)) {
+    auto load_q = [&](const Unit &u, auto &to) __attribute__((always_inline)) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            m[rb] = kMinusHuge;
-            lsum[rb] = 0.f;
-#pragma unroll
-            for (int db = 0; db < C::kDB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
             const bool is = row_q[rb] < u.n;
             const elem *row = a.Q + (u.first + (is ? row_q[rb] : 0)) * a.q_stride_t +
                               (u.h * G + (is ? row_h[rb] : 0)) * a.q_stride_h;
@@ -209,8 +211,23 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
             for (int s = 0; s < C::kSteps; ++s) {
                 // (e4m3: a lane's 16 bytes of K are 16 columns, which make two steps)
                 const int col = E8 ? s / 2 * 64 + g * 16 + s % 2 * 8 : s * 32 + g * 8;
-                q[rb][s] = as_elem8(ld_row16(row, col, Dr));
+                to[rb][s] = as_elem8(ld_row16(row, col, Dr));
             }
+        }
+    };
+    auto begin_unit = [&](const Unit &u) __attribute__((always_inline)) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            m[rb] = kMinusHuge;
+            lsum[rb] = 0.f;
+#pragma unroll
+            for (int db = 0; db < C::kDB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int s = 0; s < C::kSteps; ++s) q[0][s] = next_q[0][s];
+        } else {
+            load_q(u, q);
         }
     };
     auto compute = [&](const Unit &u, const Pages &p, int buf, const Scales &sc) __attribute__((always_inline)) {
@@ -398,17 +415,15 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         u.h = 0;
         do {
             ++u.b;
-            if (u.b < B) load_seq(u);
+            if (u.b < B) set_seq(u, paged_seq_scalar(a.b, u.b));
         } while (u.b < B && u.tiles == 0);
         return u;
     };
 
     // ---- the span
-    Pages nx_pages = pages_of(nx);
-    Scales sc[2] = {};
-    issue(nx, nx_pages, 0, sc[0]);
     Unit cur = nx;
     Pages cur_pages = nx_pages;
+    if constexpr (kAhead) load_q(cur, next_q);
     begin_unit(cur);
     bool from_start = cur.t == 0;
     int buf = 0;
@@ -417,10 +432,11 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         nx_pages = pages_of(nx);
     }
     while (true) {
-        Scales nsc = {};
+        Scales next_sc = {};
         if (todo > 1) {
-            issue(nx, nx_pages, buf ^ 1, nsc);
+            issue(nx, nx_pages, buf ^ 1, next_sc);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * KP) : "memory");
+            if constexpr (kAhead) if (nx.t == 0) load_q(nx, next_q);
         } else {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
@@ -430,7 +446,7 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
             nn = advance(nx);
             nn_pages = pages_of(nn);
         }
-        compute(cur, cur_pages, buf, sc[0]);
+        compute(cur, cur_pages, buf, sc);
         const bool to_end = cur.t + 1 == cur.tiles;
         if (to_end || todo == 1) {
             end_unit(cur, from_start, to_end, buf);
@@ -443,7 +459,7 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         cur_pages = nx_pages;
         nx = nn;
         nx_pages = nn_pages;
-        sc[0] = nsc;
+        sc = next_sc;
         buf ^= 1;
     }
 }

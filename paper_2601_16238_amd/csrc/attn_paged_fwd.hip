@@ -1,4 +1,4 @@
-// Attention over the paged key/value cache (include/attn_paged.h): which kernels a call takes.
+// Attention over the paged key/value cache (include/attn_paged.h): which kernel a call takes.
 #include "attn_paged.hpp"
 
 #include <algorithm>
@@ -12,27 +12,22 @@ PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, in
     p.kernel_d = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     const int G = Hq / Hkv, most = p.kernel_d == 256 ? 32 : 64;
     const int64_t rows = (int64_t)max_q * G;
-    p.chunks = rows > most;
-    // (next to long sequences: those of one new token, or as many as fit beside it)
-    p.decode_rows = !p.chunks ? (int)rows : G <= 16 ? 16 : G <= 32 ? 32 : G <= most ? most : 0;
-    if (p.decode_rows) {
+    if (rows <= most) {
+        p.decode_rows = (int)rows;
         const int tile = p.kernel_d == 256 && !e4m3 ? 64 : 128;
         const int64_t tiles = (keys + tile - 1) / tile;
-        if (tiles > kDecodeSpan) {
-            const int lds = p.kernel_d * (e4m3 ? 1 : 2) * 64 * 2 * (tile / 32), per_cu = 160 * 1024 / (lds + 4096);
-            p.decode_workers = (int)std::min<int64_t>(256 * std::min(per_cu, 2),
-                                                      B * Hkv * ((tiles + kDecodeSpan - 1) / kDecodeSpan));
-            p.decode_bytes = paged_span_bytes(p.decode_workers, p.decode_rows <= 16 ? 16 : p.decode_rows <= 32 ? 32 : 64,
-                                              p.kernel_d);
-        }
+        if (tiles <= kDecodeSpan) return p;
+        const int lds = p.kernel_d * (e4m3 ? 1 : 2) * 64 * 2 * (tile / 32), per_cu = 160 * 1024 / (lds + 4096);
+        p.workers = (int)std::min<int64_t>(256 * std::min(per_cu, 2), B * Hkv * ((tiles + kDecodeSpan - 1) / kDecodeSpan));
+        p.bytes = paged_span_bytes(p.workers, rows <= 16 ? 16 : rows <= 32 ? 32 : 64, p.kernel_d);
+        return p;
     }
-    p.bytes = p.decode_bytes;
-    if (p.chunks) {
-        // units of 128 rows, at most: of every sequence one that is not full
-        const int64_t units = (T * G / 128 + std::min<int64_t>(B, T * G / (p.decode_rows + 1))) * Hkv, tiles = (keys + 63) / 64;
-        p.chunk_workers = (int)std::min<int64_t>(p.kernel_d == 256 ? 256 : 512, units * ((tiles + kChunkSpan - 1) / kChunkSpan));
-        p.bytes += paged_span_bytes(p.chunk_workers, 128, p.kernel_d);
-    }
+    // A batch that may hold long sequences: all of it by the kernel of many rows, also the sequences of one token next
+    // to a chunk, which are bound by their keys' way from memory there as well, while the chunk's products run.
+    // (units of 128 rows, at most: of every sequence one that is not full)
+    const int64_t units = (T * G / 128 + std::min(B, T)) * Hkv, tiles = (keys + 63) / 64;
+    p.workers = (int)std::min<int64_t>(p.kernel_d == 256 ? 256 : 512, units * ((tiles + kChunkSpan - 1) / kChunkSpan));
+    p.bytes = paged_span_bytes(p.workers, 128, p.kernel_d);
     return p;
 }
 #endif
@@ -41,12 +36,9 @@ int launch_paged_fwd(const PagedFwdArgs &a, hipStream_t st)
 {
     const PagedPlan p = paged_plan(a.b.T, a.b.B, a.Hq, a.Hkv, a.Dr, a.max_q, (int64_t)a.b.table_width << a.b.page_shift,
                                    a.k_scale != nullptr);
-    if (p.decode_rows && launch_paged_decode(a, p.kernel_d, p.decode_rows, a.workspace ? p.decode_workers : 0, st) != 0)
-        return -1;
-    if (p.chunks)
-        return launch_paged_chunk(a, p.kernel_d, p.decode_rows, a.workspace ? p.chunk_workers : 0,
-                                  (char *)a.workspace + p.decode_bytes, st);
-    return 0;
+    const int workers = a.workspace ? p.workers : 0;
+    return p.decode_rows ? launch_paged_decode(a, p.kernel_d, p.decode_rows, workers, st)
+                         : launch_paged_chunk(a, p.kernel_d, workers, st);
 }
 
 }  // namespace attn
