@@ -259,11 +259,11 @@ template <int D, int PAR>
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedFwdArgs a, const PagedSlots<elem> s, const int R)
 {
     constexpr int kCols = D / 4, kRows = 256 / kCols / PAR, kPieces = 64;
-    __shared__ float ms[kPieces][kRows], ls[kPieces][kRows];
+    __shared__ float ms[PAR > 1 ? 1 : kPieces][kRows], ls[PAR > 1 ? 1 : kPieces][kRows];
     __shared__ f32x4 sum[PAR > 1 ? PAR : 1][PAR > 1 ? kCols : 1];
     static_assert(PAR == 1 || kRows == 1, "one row, or one thread for all pieces");
     const PagedJoin j = s.join[blockIdx.x];
-    const int tid = threadIdx.x, c = tid % kCols, p = PAR > 1 ? tid / kCols : 0, rr = PAR > 1 ? 0 : tid / kCols;
+    const int tid = threadIdx.x, l = tid & 63, c = tid % kCols, p = PAR > 1 ? tid / kCols : 0, rr = PAR > 1 ? 0 : tid / kCols;
     const int r0 = blockIdx.y * kRows, r = r0 + rr;
     if (j.pieces == 0 || r0 >= j.rows) return;
     auto at = [&](int i, int row) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0)) * R + row; };
@@ -272,32 +272,44 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedFwdArgs
     float top = kJoinMinusHuge, all = 0.f;
     for (int i0 = 0; i0 < j.pieces; i0 += kPieces) {
         const int n = min(j.pieces - i0, kPieces);
-        if (i0) __syncthreads();
-        for (int k = tid; k < n * kRows; k += 256) {
-            const int i = k / kRows, row = k % kRows;
-            const bool is = r0 + row < j.rows;
-            ms[i][row] = is ? s.m[at(i0 + i, r0 + row)] : 0.f;
-            ls[i][row] = is ? s.l[at(i0 + i, r0 + row)] : 0.f;
+        float to = top, weight = 0.f, sums = 0.f;
+        if constexpr (PAR > 1) {
+            // one row: a piece a lane, in every wave
+            const bool is = l < n;
+            const float m = is ? s.m[at(i0 + l, r0)] : kJoinMinusHuge, sum_l = is ? s.l[at(i0 + l, r0)] : 0.f;
+            to = fmaxf(to, m);
+#pragma unroll
+            for (int d = 32; d; d /= 2) to = fmaxf(to, __shfl_xor(to, d));
+            weight = fast_exp2(m - to);
+            sums = sum_l * weight;
+#pragma unroll
+            for (int d = 32; d; d /= 2) sums += __shfl_xor(sums, d);
+        } else {
+            if (i0) __syncthreads();
+            for (int k = tid; k < n * kRows; k += 256) {
+                const int i = k / kRows, row = k % kRows;
+                const bool is = r0 + row < j.rows;
+                ms[i][row] = is ? s.m[at(i0 + i, r0 + row)] : 0.f;
+                ls[i][row] = is ? s.l[at(i0 + i, r0 + row)] : 0.f;
+            }
+            __syncthreads();
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) to = fmaxf(to, ms[i][rr]);
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) sums += ls[i][rr] * fast_exp2(ms[i][rr] - to);
         }
-        __syncthreads();
-        float to = top;
-        for (int i = 0; i < n; ++i) to = fmaxf(to, ms[i][rr]);
         const float keep = fast_exp2(top - to);
         x *= keep;
-        all *= keep;
+        all = all * keep + sums;
         top = to;
-        for (int i = 0; i < n; ++i) all += ls[i][rr] * fast_exp2(ms[i][rr] - to);
-        if (mine) {
-            const float *part = s.part + at(i0 + p, r) * D + 4 * c;
-            const int64_t step = 2 * (int64_t)PAR * R * D;
-            int i = p;
-            if (i0 == 0 && i == 0) {  // (the first piece lies in its worker's other slot)
-                x += *(const f32x4 *)part * fast_exp2(ms[0][rr] - to);
-                part = s.part + at(PAR, r) * D + 4 * c;
-                i = PAR;
-            }
+        // (the first piece lies in its worker's other slot)
+        const float *const part = s.part + at(i0, r) * D + 4 * c;
+        const int64_t step = 2 * (int64_t)R * D, back = i0 == 0 ? (int64_t)R * D : 0;
 #pragma unroll 4
-            for (; i < n; i += PAR, part += step) x += *(const f32x4 *)part * fast_exp2(ms[i][rr] - to);
+        for (int i = 0; i < n; i += PAR) {
+            const int k = i + p;
+            const float by = PAR > 1 ? __shfl(weight, k & 63) : fast_exp2(ms[PAR > 1 ? 0 : k][rr] - to);
+            if (k < n && mine) x += *(const f32x4 *)(part + k * step - (k ? back : 0)) * by;
         }
     }
     if constexpr (PAR > 1) {

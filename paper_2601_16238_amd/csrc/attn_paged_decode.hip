@@ -71,6 +71,10 @@ __device__ __forceinline__ int decode_tiles(const PagedSeq &s, int G, int max_ro
     return s.n < 1 || (int64_t)s.n * G > max_rows ? 0 : max(1, (s.len + TK - 1) / TK);
 }
 
+// What the end of a unit counts as, in tiles: the waves wait for each other there.  (Without it the spans of short
+// sequences, which end many, were the last to be done.)
+constexpr int kUnitEnd = 1;
+
 // SPLIT: work-groups with spans, partial results in the workspace.  Otherwise one work-group for each sequence and K/V head.
 template <int D, int RB, bool E8, bool SPLIT>
 __global__ void __launch_bounds__((DecodeCfg<D, E8>::kThreads))
@@ -96,26 +100,43 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         u.tiles = decode_tiles(s, G, max_rows, TK);
     };
     Unit nx;
-    int todo;  // tiles of the span that are not computed yet
+    int left;  // of the span, from the tile nx on
+    auto next_unit = [&](Unit &u) __attribute__((always_inline)) {
+        u.t = 0;
+        if (++u.h < Hkv) return;
+        u.h = 0;
+        do {
+            ++u.b;
+            if (u.b < B) set_seq(u, paged_seq_scalar(a.b, u.b));
+        } while (u.b < B && u.tiles == 0);
+    };
     PagedSpan span = {};
     if constexpr (SPLIT) {
         span = paged_span<NW>(a.b, Hkv, blockIdx.x, gridDim.x, kDecodeSpan, scan,
-                              [&](const PagedSeq &s) { return decode_tiles(s, G, max_rows, TK); });
-        todo = span.left;
+                              [&](const PagedSeq &s) {
+            const int tiles = decode_tiles(s, G, max_rows, TK);
+            return tiles ? tiles + kUnitEnd : 0;
+        });
         if (tid == 0) slots.join[blockIdx.x].pieces = 0;
-        if (todo == 0) return;
+        if (span.left == 0) return;
         nx.b = span.b;
         set_seq(nx, span.seq);
         const int in = __builtin_amdgcn_readfirstlane((int)(span.begin - span.front));
-        nx.h = in / nx.tiles;
-        nx.t = in - nx.h * nx.tiles;
+        nx.h = in / (nx.tiles + kUnitEnd);
+        nx.t = in - nx.h * (nx.tiles + kUnitEnd);
+        left = span.left;
+        if (nx.t >= nx.tiles) {  // it begins with the end of a unit
+            left -= nx.tiles + kUnitEnd - nx.t;
+            if (left <= 0) return;
+            next_unit(nx);
+        }
     } else {
         nx.b = blockIdx.x / Hkv;
         nx.h = blockIdx.x % Hkv;
         nx.t = 0;
         set_seq(nx, paged_seq_scalar(a.b, nx.b));
-        todo = nx.tiles;
-        if (todo == 0) return;
+        left = nx.tiles;
+        if (left == 0) return;
     }
 
     // ---- lanes
@@ -408,32 +429,26 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         }
     };
 
-    auto advance = [&](Unit u) __attribute__((always_inline)) {
-        if (++u.t < u.tiles) return u;
-        u.t = 0;
-        if (++u.h < Hkv) return u;
-        u.h = 0;
-        do {
-            ++u.b;
-            if (u.b < B) set_seq(u, paged_seq_scalar(a.b, u.b));
-        } while (u.b < B && u.tiles == 0);
-        return u;
-    };
-
-    // ---- the span
+    // ---- the span: tile cur, whose transfers are on their way; nx behind it, which the span may not hold any more
     Unit cur = nx;
     Pages cur_pages = nx_pages;
     if constexpr (kAhead) load_q(cur, next_q);
     begin_unit(cur);
     bool from_start = cur.t == 0;
     int buf = 0;
-    if (todo > 1) {
-        nx = advance(cur);
-        nx_pages = pages_of(nx);
-    }
+    // u and what is left of the span to the tile behind it
+    auto advance = [&](Unit &u) __attribute__((always_inline)) {
+        --left;
+        if (++u.t < u.tiles) return;
+        left -= SPLIT ? kUnitEnd : left;
+        if (left > 0) next_unit(u);
+    };
+    advance(nx);
+    bool more = left > 0;
+    if (more) nx_pages = pages_of(nx);
     while (true) {
         Scales next_sc = {};
-        if (todo > 1) {
+        if (more) {
             issue(nx, nx_pages, buf ^ 1, next_sc);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * KP) : "memory");
             if constexpr (kAhead) if (nx.t == 0) load_q(nx, next_q);
@@ -442,19 +457,21 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         }
         Unit nn = nx;
         Pages nn_pages = nx_pages;
-        if (todo > 2) {
-            nn = advance(nx);
-            nn_pages = pages_of(nn);
+        bool still = false;
+        if (more) {
+            advance(nn);
+            still = left > 0;
+            if (still) nn_pages = pages_of(nn);
         }
         compute(cur, cur_pages, buf, sc);
         const bool to_end = cur.t + 1 == cur.tiles;
-        if (to_end || todo == 1) {
+        if (to_end || !more) {
             end_unit(cur, from_start, to_end, buf);
-            if (todo == 1) return;
+            if (!more) return;
             begin_unit(nx);
             from_start = true;
         }
-        --todo;
+        more = still;
         cur = nx;
         cur_pages = nx_pages;
         nx = nn;
