@@ -2,8 +2,11 @@
 //
 // The rows of a unit of work are kBR = 32 NW consecutive ones of a sequence and K/V head, new token by new token and
 // within it query head by query head, so that a tile of 64 keys is read once for all heads that share it; a wave has
-// 32 of them.  S^T = K Q^T and O^T += V^T P^T by 32x32x16 MFMA with the scores of a query in one lane; K and V tiles
-// reach LDS row-major, two buffers each.  16-bit tiles come by direct transfers, 16 rows (of one page) to a buffer
+// 32 of them.  S^T = K Q^T and O^T += V^T P^T by 32x32x16 MFMA with the scores of a query in one lane.  A
+// step forms the scores of 32 keys, the probabilities of the 32 before them and the products with V of the 32 before
+// those: three independent pieces of work in one block of code, so that the matrix pipe and the vector ALU overlap inside
+// a wave.  K and V tiles reach LDS row-major, two buffers each: two steps share a pair of tiles of 64 keys, K's 32 keys
+// ahead of the probabilities and V's 32 behind.  16-bit tiles come by direct transfers, 16 rows (of one page) to a buffer
 // resource; slots behind the last key, pages that are none and columns that do not exist read as zero.  e4m3 tiles
 // pass through registers, where they are converted once for all waves: K exactly, V with its power of two; what is
 // left of V's scale is added to the exponent of the probabilities and taken out of their sums.
@@ -150,73 +153,75 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     constexpr uint32_t kPast = 1u << 31;
     const uint32_t lds0 = lds_address(smem);
     const uint32_t voff = L::lane_offset(l, row_bytes, Dr, kPast);
-    struct Tile { int id[4]; float k[4], v[4]; };  // pages of its 16-key groups, and their scales
-    auto ids_of = [&](int kt, Tile &t) __attribute__((always_inline)) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int key = kt * BC + 16 * g;
-            int id = key < s.len ? scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride +
-                                               (key >> a.b.page_shift)) : -1;
-            if (!a.b.is_page(id)) id = -1;
-            t.id[g] = id;
-            if constexpr (E8) {
-                t.k[g] = id < 0 ? 1.f : scalar_load(a.k_scale + (int64_t)id * Hkv + u.h);
-                t.v[g] = id < 0 ? 1.f : scalar_load(a.v_scale + (int64_t)id * Hkv + u.h);
+    // Set j: the groups 4 j + 2 .. 4 j + 5 of 16 keys each, counted from the unit's first key that the span has; they are
+    // K's tile j and V's tile j + 1.  Wave w fetches group w, and tells the others what its scores are multiplied with, what
+    // is added to the exponents of its probabilities (minus infinity: no page, or behind the last key) and what their
+    // sum is multiplied with.
+    struct Const { float c, rest, inv, unused; };
+    __shared__ Const consts[2][4];
+    int key0 = 0, key1 = 0;  // the keys of the unit that the span has
+    auto key_of = [&](int j, int g) { return key0 + 64 * j + 32 + 16 * g; };
+    auto id_of = [&](int j) __attribute__((always_inline)) {
+        const int key = key_of(j, w);
+        return key >= key0 && key < key1 ? scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride +
+                                                       (key >> a.b.page_shift)) : -1;
+    };
+    // the wave's group: offset of its first row in the cache, bytes that exist of it, and its scales
+    struct Group { int64_t off; uint32_t bytes; float k, v; };
+    auto group_of = [&](int j, int id) __attribute__((always_inline)) {
+        const bool is = a.b.is_page(id);
+        const int key = key_of(j, w), page = is ? id : 0;
+        Group t;
+        t.bytes = is ? (uint32_t)(min(s.len - key, 16) - 1) * row_bytes + Dr * (E8 ? 1 : 2) : 0;
+        t.off = (page * a.cache_stride_p + u.h * a.cache_stride_h + (key & (a.b.page_size() - 1)) * a.cache_stride_s) *
+                (E8 ? 1 : 2);
+        if constexpr (E8) {
+            t.k = is ? scalar_load(a.k_scale + (int64_t)page * Hkv + u.h) : 1.f;
+            t.v = is ? scalar_load(a.v_scale + (int64_t)page * Hkv + u.h) : 1.f;
+        }
+        return t;
+    };
+    auto tell = [&](int j, const Group &t) __attribute__((always_inline)) {
+        Const x = {a.scale_log2e, t.bytes ? 0.f : -INFINITY, 1.f, 0.f};
+        if constexpr (E8) {
+            // (not 0, which a masked score would turn into NaN)
+            x.c = fmaxf(a.scale_log2e * t.k, 1e-38f);
+            const float left = scale_rest(t.v);
+            if (t.bytes && left > 0.f) {
+                x.rest = fast_log2(left);
+                x.inv = 1.f / left;
             }
         }
+        if (l == 0) consts[j & 1][w] = x;
     };
-    // group g of tile kt: offset of its first row in the cache, and the bytes that exist of it
-    auto place = [&](int kt, int id, int g, uint32_t &bytes) __attribute__((always_inline)) {
-        const int key = kt * BC + 16 * g, rows = id < 0 ? 0 : min(s.len - key, 16);
-        bytes = rows > 0 ? (uint32_t)(rows - 1) * row_bytes + Dr * (E8 ? 1 : 2) : 0;
-        return ((int64_t)(id < 0 ? 0 : id) * a.cache_stride_p + u.h * a.cache_stride_h +
-                (key & (a.b.page_size() - 1)) * a.cache_stride_s) * (E8 ? 1 : 2);
+    // piece n of the wave's rows of a 16-bit tile of K (tensor 0) or V
+    auto transfer = [&](int tensor, desc_t d, int buf, int n) __attribute__((always_inline)) {
+        if constexpr (!E8)
+            dma16_between(d, lds0 + (tensor ? C::kOffV : 0) + buf * C::kTile + L::base(w * C::kPerWave + n), voff,
+                          n * L::kRows * row_bytes);
     };
-    auto transfer = [&](int kt, const Tile &t, int buf) __attribute__((always_inline)) {
-        if constexpr (!E8) {
-#pragma unroll
-            for (int n = 0; n < C::kPerWave; ++n) {
-                const int ii = w + n * NW, row0 = ii * L::kRows, g = n * NW * L::kRows / 16 + (w * L::kRows) / 16;
-                uint32_t bytes;
-                // (which group: known when compiled but for D = 64, where a wave's is its own)
-                const int id = D == 64 ? (g == 0 ? t.id[0] : g == 1 ? t.id[1] : g == 2 ? t.id[2] : t.id[3])
-                                       : t.id[n * NW * L::kRows / 16];
-                const int64_t off = place(kt, id, g, bytes);
-                const uint32_t soff = (row0 & 15) * row_bytes, lds = lds0 + buf * C::kTile + L::base(ii);
-                dma16_between(make_desc((const char *)a.K_cache + off, bytes), lds, voff, soff);
-                dma16_between(make_desc((const char *)a.V_cache + off, bytes), lds + C::kOffV, voff, soff);
-            }
-        }
+    auto desc_of = [&](int tensor, const Group &t) __attribute__((always_inline)) {
+        return make_desc((const char *)(tensor ? a.V_cache : a.K_cache) + t.off, t.bytes);
     };
-    // e4m3: 16 codes a thread and step, of row (w + NW j) kBC / ..; a wave's rows lie in one group
+    // e4m3: 16 codes a thread and step
     constexpr int RPW = 64 / C::kChunks;  // rows of a wave's step
-    u32x4 ck[E8 ? C::kPerThread : 1], cv[E8 ? C::kPerThread : 1];
-    auto fetch = [&](int kt, const Tile &t) __attribute__((always_inline)) {
+    u32x4 codes[E8 ? C::kPerThread : 1];
+    const uint32_t at8 = l % C::kChunks * 16 < Dr ? l / C::kChunks * row_bytes + l % C::kChunks * 16 : kPast;
+    auto fetch = [&](int tensor, const Group &t) __attribute__((always_inline)) {
         if constexpr (E8) {
+            const rsrc_t d = make_rsrc((const char *)(tensor ? a.V_cache : a.K_cache) + t.off, t.bytes);
 #pragma unroll
-            for (int j = 0; j < C::kPerThread; ++j) {
-                const int row0 = (w + NW * j) * RPW, g = row0 / 16;
-                uint32_t bytes;
-                const int id = g == 0 ? t.id[0] : g == 1 ? t.id[1] : g == 2 ? t.id[2] : t.id[3];
-                const int64_t off = place(kt, id, g, bytes);
-                const int c = l % C::kChunks;
-                const uint32_t at = c * 16 < Dr ? (row0 % 16 + l / C::kChunks) * row_bytes + c * 16 : kPast;
-                ck[j] = buf_load16(make_rsrc((const char *)a.K_cache + off, bytes), at, 0);
-                cv[j] = buf_load16(make_rsrc((const char *)a.V_cache + off, bytes), at, 0);
-            }
+            for (int n = 0; n < C::kPerThread; ++n) codes[n] = buf_load16(d, at8, n * RPW * row_bytes);
         }
     };
-    auto convert = [&](const Tile &t, int buf) __attribute__((always_inline)) {
+    auto convert = [&](int tensor, float by, int buf) __attribute__((always_inline)) {
         if constexpr (E8) {
 #pragma unroll
-            for (int j = 0; j < C::kPerThread; ++j) {
-                const int row0 = (w + NW * j) * RPW, g = row0 / 16, row = row0 + l / C::kChunks, c = l % C::kChunks;
-                const float sv = g == 0 ? t.v[0] : g == 1 ? t.v[1] : g == 2 ? t.v[2] : t.v[3];
-                char *const k = smem + buf * C::kTile;
-                *(elem8 *)(k + L::at(row, 2 * c)) = from_e4m3(ck[j].x, ck[j].y, 1.f, 1.f);
-                *(elem8 *)(k + L::at(row, 2 * c + 1)) = from_e4m3(ck[j].z, ck[j].w, 1.f, 1.f);
-                *(elem8 *)(k + C::kOffV + L::at(row, 2 * c)) = from_e4m3(cv[j].x, cv[j].y, sv, sv);
-                *(elem8 *)(k + C::kOffV + L::at(row, 2 * c + 1)) = from_e4m3(cv[j].z, cv[j].w, sv, sv);
+            for (int n = 0; n < C::kPerThread; ++n) {
+                const int row = 16 * w + n * RPW + l / C::kChunks, c = l % C::kChunks;
+                char *const to = smem + (tensor ? C::kOffV : 0) + buf * C::kTile;
+                *(elem8 *)(to + L::at(row, 2 * c)) = from_e4m3(codes[n].x, codes[n].y, by, by);
+                *(elem8 *)(to + L::at(row, 2 * c + 1)) = from_e4m3(codes[n].z, codes[n].w, by, by);
             }
         }
     };
@@ -237,11 +242,26 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         // ... and the wave's first row (all see that many)
         const int all_see = causal ? __builtin_amdgcn_readfirstlane(min(s.len - s.n + (u.rt * BR + w * 32) / G, s.len - 1))
                                    : s.len - 1;
-        Tile cur, next;
-        ids_of(t0, cur);
-        transfer(t0, cur, 0);
-        fetch(t0, cur);
-        // the unit's rows of Q to the second buffers, in the layout of the tiles: 64 in K's, 64 in V's
+        key0 = t0 * BC;
+        key1 = min(t1 * BC, s.len);
+        const int T = t1 - t0;
+        // First the 32 keys of sub-tile 0, as the second half of K's "tile -1" and of V's tile 0, and the unit's rows of Q
+        // to the second buffers, in the layout of the tiles: 64 in K's, 64 in V's.
+        Group now = group_of(-1, id_of(-1)), next = group_of(0, id_of(0));  // of sets j, j + 1
+        int ahead = id_of(1);                                               // of set j + 2
+        tell(-1, now);
+        tell(0, next);
+        {
+            const desc_t Kd = desc_of(0, now), Vd = desc_of(1, now);
+#pragma unroll
+            for (int n = 0; n < C::kPerWave; ++n) {
+                transfer(0, Kd, 0, n);
+                transfer(1, Vd, 0, n);
+            }
+        }
+        fetch(0, now);
+        convert(0, 1.f, 0);
+        fetch(1, now);
         {
             constexpr int CPR = D / 8;
 #pragma unroll
@@ -254,7 +274,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                 *(u32x4 *)(smem + C::kTile + (qr >> 6) * C::kOffV + L::at(qr & 63, c)) = x;
             }
         }
-        convert(cur, 0);
+        convert(1, now.v, 0);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         elem8 qf[KS];
@@ -264,97 +284,162 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const elem8 *)(Qs + L::step(ks));
         }
         float m = kChunkMinusHuge, lsum = 0.f;
-        f32x16 o[DB];
+        f32x16 o[DB], sa, sb;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sa[i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sa = mfma32(*(const elem8 *)(smem + C::kHalf + L::step(ks) + k_lane), qf[ks], sa);
+        __syncthreads();  // Q and K's "tile -1" are read
+        {
+            const desc_t Kd = desc_of(0, next);
+#pragma unroll
+            for (int n = 0; n < C::kPerWave; ++n) transfer(0, Kd, 0, n);
+        }
+        fetch(0, next);
+        convert(0, 1.f, 0);
+        elem8 pp[2];  // probabilities of the sub-tile before
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pp[0][i] = pp[1][i] = (elem)0.f;
 
-        if (t0 + 1 < t1) ids_of(t0 + 1, next);
-        for (int kt = t0; kt < t1; ++kt) {
-            const int buf = (kt - t0) & 1;
-            // (the other buffers' last reads, of Q or tile kt - 1, are done)
-            __syncthreads();
-            if (kt + 1 < t1) {
-                transfer(kt + 1, next, buf ^ 1);
-                fetch(kt + 1, next);
+        constexpr int NS = KS / 4, NP = 2 * NS;  // phases of four products: with K, with V
+        elem8 f[2][4];
+        // (per-lane LDS addresses of the current tiles, opaque to the compiler, so that step and block are folded into the
+        // immediate offsets of the LDS instructions)
+        int k_base = 0, v_base0 = 0, v_base1 = 0;
+        auto set_bases = [&](int buf) __attribute__((always_inline)) {
+            k_base = k_lane + buf * C::kTile;
+            v_base0 = v_lane[0] + buf * C::kTile;
+            v_base1 = v_lane[1] + buf * C::kTile;
+            asm volatile("" : "+v"(k_base), "+v"(v_base0), "+v"(v_base1));
+        };
+        auto load = [&](int half, int p, elem8 (&to)[4]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if (p < NS) {
+                    to[t] = *(const elem8 *)(smem + half * C::kHalf + L::step(4 * p + t) + k_base);
+                } else {
+                    const int i = 4 * (p - NS) + t;
+                    const char *x = smem + (2 * half + i / DB) * L::kRows16 + i % DB * L::kBlock;
+                    to[t] = join8(lds_read_tr((const elem *)(x + v_base0)), lds_read_tr((const elem *)(x + v_base1)));
+                }
             }
-            const char *Kt = smem + buf * C::kTile;
+        };
+        // Step `half` of tile j: probabilities of sub-tile 2 j + half (scores in x), scores of the next into y, V times the
+        // probabilities of the one before.  Between the products of the first step the next tiles are requested (in one
+        // burst, the waves would all queue at the compute unit's vector-memory path while the matrix pipes idle).
+        struct Pair { float c[2], rest[2], inv[2]; };  // of a sub-tile's two groups
+        auto pair_of = [&](int j, int g) __attribute__((always_inline)) {
+            Pair t;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                f32x16 x;
+            for (int i = 0; i < 2; ++i) {
+                const Const x = consts[j & 1][g + i];
+                t.c[i] = E8 ? pin_scalar(x.c) : a.scale_log2e;
+                t.rest[i] = pin_scalar(x.rest);
+                t.inv[i] = E8 ? pin_scalar(x.inv) : 1.f;
+            }
+            return t;
+        };
+        desc_t Kd, Vd;
+        auto step = [&](bool masked, int half, int kb, int fill, const Pair &t, f32x16 &x, f32x16 &y)
+                        __attribute__((always_inline)) {
+            if (masked) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = 0.f;
+                for (int i = 0; i < 16; ++i)
+                    if (acc_row(i, h) > seen - kb) x[i] = -INFINITY;
+            }
+            float e[16], part[2] = {0.f, 0.f}, off[2] = {t.rest[0] - m, t.rest[1] - m};
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    x = mfma32(*(const elem8 *)(Kt + half * C::kHalf + L::step(ks) + k_lane), qf[ks], x);
-                float c[2] = {a.scale_log2e, a.scale_log2e}, rest[2] = {0.f, 0.f}, inv[2] = {1.f, 1.f};
-                if constexpr (E8)
+            for (int i = 0; i < 16; ++i) y[i] = 0.f;
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        // (not 0, which a masked score would turn into NaN)
-                        c[g] = fmaxf(c[g] * cur.k[2 * half + g], 1e-38f);
-                        const float left = scale_rest(cur.v[2 * half + g]);
-                        rest[g] = left > 0.f ? fast_log2(left) : 0.f;
-                        inv[g] = left > 0.f ? 1.f / left : 1.f;
-                    }
-                const int kb = kt * BC + 32 * half;
-                if (kb + 31 > all_see || cur.id[2 * half] < 0 || cur.id[2 * half + 1] < 0) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int key = acc_row(i, h);
-                        if (key > seen - kb || cur.id[2 * half + (i >= 8)] < 0) x[i] = -INFINITY;
-                    }
+            for (int p = 0; p < NP; ++p) {
+                if (p + 1 < NP) load(half, p + 1, f[(p + 1) & 1]);
+                else if (half == 0) load(1, 0, f[0]);
+                if (half == 0) {
+                    static_assert(C::kPerWave == NP, "a piece of K and of V a phase");
+                    transfer(0, Kd, fill, p);
+                    transfer(1, Vd, fill, p);
                 }
-                float e[16], part[2];
-                auto probs = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        part[g] = 0.f;
-#pragma unroll
-                        for (int i = 8 * g; i < 8 * g + 8; ++i) {
-                            e[i] = fast_exp2(__builtin_fmaf(x[i], c[g], rest[g] - m));
-                            part[g] += e[i];
-                        }
-                    }
-                };
-                probs();
-                if (__builtin_amdgcn_ballot_w64(part[0] + part[1] > kChunkOverflow)) {
-                    float t[2];
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        t[g] = x[8 * g];
-#pragma unroll
-                        for (int i = 1; i < 8; ++i) t[g] = fmaxf(t[g], x[8 * g + i]);
-                        t[g] *= c[g];
-                    }
-                    const float to = fmaxf(m, xhalf_max(fmaxf(t[0], t[1]))), alpha = fast_exp2(m - to);
-                    m = to;
-                    lsum *= alpha;
-#pragma unroll
-                    for (int db = 0; db < DB; ++db)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-                    probs();
+                for (int k = 0; k < 4; ++k) {
+                    const int n = 4 * (p - NS) + k;
+                    if (p < NS) y = mfma32(f[p & 1][k], qf[4 * p + k], y);
+                    else o[n % DB] = mfma32(f[p & 1][k], pp[n / DB], o[n % DB]);
                 }
-                lsum += E8 ? part[0] * inv[0] + part[1] * inv[1] : part[0] + part[1];
+#pragma unroll
+                for (int i = 16 * p / NP; i < 16 * (p + 1) / NP; ++i) {
+                    e[i] = fast_exp2(__builtin_fmaf(x[i], t.c[i >= 8], off[i >= 8]));
+                    part[i >= 8] += e[i];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(part[0] + part[1] > kChunkOverflow) != 0, 0)) {
+                // a probability has outgrown the reference maximum (always the first ones): it moves to the running maximum
+                float top[2];
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    const elem8 p = pack8(e[8 * g], e[8 * g + 1], e[8 * g + 2], e[8 * g + 3], e[8 * g + 4], e[8 * g + 5],
-                                          e[8 * g + 6], e[8 * g + 7]);
-                    const char *Vt = Kt + (2 * half + g) * L::kRows16;
+                    top[g] = x[8 * g];
 #pragma unroll
-                    for (int db = 0; db < DB; ++db)
-                        o[db] = mfma32(join8(lds_read_tr((const elem *)(Vt + db * L::kBlock + v_lane[0])),
-                                             lds_read_tr((const elem *)(Vt + db * L::kBlock + v_lane[1]))), p, o[db]);
+                    for (int i = 1; i < 8; ++i) top[g] = fmaxf(top[g], x[8 * g + i]);
+                    top[g] = top[g] * t.c[g] + t.rest[g];
+                }
+                const float to = fmaxf(m, xhalf_max(fmaxf(top[0], top[1]))), alpha = fast_exp2(m - to);
+                m = to;
+                lsum *= alpha;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+                part[0] = part[1] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    e[i] = fast_exp2(__builtin_fmaf(x[i], t.c[i >= 8], t.rest[i >= 8] - m));
+                    part[i >= 8] += e[i];
                 }
             }
-            if (kt + 1 < t1) {
-                convert(next, buf ^ 1);
-                cur = next;
-                if (kt + 2 < t1) ids_of(kt + 2, next);
-            }
+            lsum += E8 ? part[0] * t.inv[0] + part[1] * t.inv[1] : part[0] + part[1];
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+                pp[g] = pack8(e[8 * g], e[8 * g + 1], e[8 * g + 2], e[8 * g + 3], e[8 * g + 4], e[8 * g + 5], e[8 * g + 6],
+                              e[8 * g + 7]);
+        };
+        Pair behind = pair_of(-1, 2);
+        now = next;
+        for (int j = 0; j < T; ++j) {
+            const int buf = j & 1;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();  // tiles j are there, and tiles j - 1 are read
+            set_bases(buf);
+            load(0, 0, f[0]);
+            const Pair first = pair_of(j, 0), second = pair_of(j, 2);
+            next = group_of(j + 1, ahead);
+            ahead = id_of(j + 2);
+            Vd = desc_of(1, now);
+            Kd = desc_of(0, next);
+            fetch(1, now);
+            tell(j + 1, next);
+            const int kb = key0 + 64 * j;
+            step(kb + 31 > all_see, 0, kb, buf ^ 1, behind, sa, sb);
+            convert(1, now.v, buf ^ 1);
+            fetch(0, next);
+            step(kb + 63 > all_see, 1, kb + 32, buf ^ 1, first, sb, sa);
+            convert(0, 1.f, buf ^ 1);
+            behind = second;
+            now = next;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        // the last probabilities' products
+        set_bases(T & 1);
+#pragma unroll
+        for (int p = 0; p < NS; ++p) {
+            load(0, NS + p, f[0]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                o[(4 * p + t) % DB] = mfma32(f[0][t], pp[(4 * p + t) / DB], o[(4 * p + t) % DB]);
         }
         __syncthreads();  // all tiles are read: the buffers take the rows of O
 
