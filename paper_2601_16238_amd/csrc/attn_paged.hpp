@@ -90,6 +90,7 @@ struct PagedPlan {
     size_t bytes;     // workspace
 };
 constexpr int kDecodeSpan = 4, kChunkSpan = 4;  // tiles of a span, at least
+constexpr int chunk_rows(int D) { return D == 128 ? 256 : 128; }  // of a unit, in the kernel of many rows
 PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3);
 
 // Rows and keys of a sequence, inside the buffers whatever device memory holds.

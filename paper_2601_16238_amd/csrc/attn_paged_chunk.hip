@@ -18,22 +18,33 @@ namespace attn {
 
 template <int D, bool E8>
 struct ChunkCfg {
-    static constexpr int kNW = 4;
+    static constexpr int kNW = D == 128 ? 8 : 4;
     static constexpr int kThreads = kNW * 64;
     static constexpr int kBR = kNW * 32;
+    static_assert(kBR == chunk_rows(D), "as planned");
     static constexpr int kBC = 64;
     using L = Pieces<D>;
     static constexpr int kPieces = kBC / L::kRows;            // transfers of a 16-bit tile
     static constexpr int kPerWave = kPieces / kNW;
     static constexpr int kTile = L::base(kPieces);            // bytes
     static constexpr int kHalf = kTile / 2;                   // 32 rows further
-    static constexpr int kOffV = 2 * kTile;
-    static constexpr int kLds = 4 * kTile;
+    static constexpr int kBufs = D == 128 && !E8 ? 3 : 2;     // of K, and of V
+    static constexpr int kOffV = kBufs * kTile;
+    static constexpr int kAreas = kNW / 2;                    // 64 rows of Q each, in the buffers that are free at first
+    static constexpr int kLds = (kAreas > 2 * (kBufs - 1) ? 2 * kBufs + kAreas - 2 * (kBufs - 1) : 2 * kBufs) * kTile;
+    static constexpr int kWaveRows = kBC / kNW;               // of a tile, fetched by a wave
+    // place of rows 64 i .. of Q
+    __device__ static int area(int i)
+    {
+        constexpr int kFree = kBufs - 1;  // of K, and of V
+        return i < kFree ? (1 + i) * kTile : i < 2 * kFree ? kOffV + (1 + i - kFree) * kTile : (2 * kBufs + i - 2 * kFree) * kTile;
+    }
     static constexpr int kChunks = D / 16;                    // 16-byte pieces of an e4m3 row
     static constexpr int kPerThread = kBC * kChunks / kThreads;
     static constexpr int kWaves = D > 128 ? 1 : 2;            // a SIMD
-    static_assert(kPieces % kNW == 0 && kBC * kChunks % kThreads == 0, "staging divides evenly");
-    static_assert(kWaves * kLds <= 160 * 1024, "LDS of a compute unit");
+    static constexpr int kPerUnit = kWaves * 4 / kNW;         // work-groups of a compute unit
+    static_assert(kPieces % kNW == 0 && kBC * kChunks % kThreads == 0 && 16 % kWaveRows == 0, "staging divides evenly");
+    static_assert(kPerUnit * kLds <= 160 * 1024, "LDS of a compute unit");
 };
 
 // Units of rows of a sequence: rt has the rows rt BR .. of the sequence's n G.
@@ -61,12 +72,17 @@ struct ChunkWalk {
         return left ? token + 1 : token;
     }
 };
+// What the beginning and end of a unit count as, in tiles: its rows come and go while the matrix pipes wait.
+#ifndef CHUNK_END
+#define CHUNK_END 4
+#endif
+constexpr int kChunkEnd = CHUNK_END;
 __device__ __forceinline__ int chunk_cost(const PagedSeq &s, int G, int max_q, int BR, bool causal)
 {
     const int row_tiles = chunk_row_tiles(s, G, max_q, BR);
     ChunkWalk walk(G, BR);
     int sum = 0;
-    for (int rt = 0; rt < row_tiles; ++rt) sum += chunk_tiles(s, causal, walk.next());
+    for (int rt = 0; rt < row_tiles; ++rt) sum += chunk_tiles(s, causal, walk.next()) + kChunkEnd;
     return sum;
 }
 
@@ -101,6 +117,19 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         s = q;
         row_tiles = chunk_row_tiles(q, G, a.max_q, BR);
     };
+    auto next_unit = [&]() __attribute__((always_inline)) {
+        u.t = 0;
+        if (++u.rt == row_tiles) {
+            u.rt = 0;
+            walk = ChunkWalk(G, BR);
+            if (++u.h == Hkv) {
+                u.h = 0;
+                do set_seq(paged_seq_scalar(a.b, ++u.b)); while (row_tiles == 0);
+            }
+        }
+        u.token = walk.next();
+        u.tiles = chunk_tiles(s, causal, u.token);
+    };
     if constexpr (SPLIT) {
         span = paged_span<NW>(a.b, Hkv, me, gridDim.x, kChunkSpan, scan,
                               [&](const PagedSeq &q) { return chunk_cost(q, G, a.max_q, BR, causal); });
@@ -111,7 +140,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         set_seq(span.seq);
         // which head, which unit of it and which of its tiles
         int cost = 0;
-        for (int rt = 0; rt < row_tiles; ++rt) cost += chunk_tiles(s, causal, walk.next());
+        for (int rt = 0; rt < row_tiles; ++rt) cost += chunk_tiles(s, causal, walk.next()) + kChunkEnd;
         int in = (int)(span.begin - span.front);
         u.h = in / cost;
         in -= u.h * cost;
@@ -120,11 +149,16 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         while (true) {
             u.token = walk.next();
             u.tiles = chunk_tiles(s, causal, u.token);
-            if (in < u.tiles) break;
-            in -= u.tiles;
+            if (in < u.tiles + kChunkEnd) break;
+            in -= u.tiles + kChunkEnd;
             ++u.rt;
         }
         u.t = in;
+        if (in >= u.tiles) {  // the span begins with the end of a unit
+            todo -= u.tiles + kChunkEnd - in;
+            if (todo <= 0) return;
+            next_unit();
+        }
     } else {
         // one work-group for each unit: row tiles of a sequence from floor(first G / BR) + b on
         const int64_t slot = blockIdx.x / Hkv;
@@ -154,15 +188,17 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     const uint32_t lds0 = lds_address(smem);
     const uint32_t voff = L::lane_offset(l, row_bytes, Dr, kPast);
     // Set j: the groups 4 j + 2 .. 4 j + 5 of 16 keys each, counted from the unit's first key that the span has; they are
-    // K's tile j and V's tile j + 1.  Wave w fetches group w, and tells the others what its scores are multiplied with, what
+    // K's tile j and V's tile j + 1.  A wave fetches rows of one group, `own`, and tells the others what its scores are multiplied with, what
     // is added to the exponents of its probabilities (minus infinity: no page, or behind the last key) and what their
     // sum is multiplied with.
+    const int own = w * C::kWaveRows / 16, own_row = w * C::kWaveRows % 16;
     struct Const { float c, rest, inv, unused; };
-    __shared__ Const consts[2][4];
+    constexpr int kSets = 4;
+    __shared__ Const consts[kSets][4];
     int key0 = 0, key1 = 0;  // the keys of the unit that the span has
     auto key_of = [&](int j, int g) { return key0 + 64 * j + 32 + 16 * g; };
     auto id_of = [&](int j) __attribute__((always_inline)) {
-        const int key = key_of(j, w);
+        const int key = key_of(j, own);
         return key >= key0 && key < key1 ? scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride +
                                                        (key >> a.b.page_shift)) : -1;
     };
@@ -170,7 +206,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     struct Group { int64_t off; uint32_t bytes; float k, v; };
     auto group_of = [&](int j, int id) __attribute__((always_inline)) {
         const bool is = a.b.is_page(id);
-        const int key = key_of(j, w), page = is ? id : 0;
+        const int key = key_of(j, own), page = is ? id : 0;
         Group t;
         t.bytes = is ? (uint32_t)(min(s.len - key, 16) - 1) * row_bytes + Dr * (E8 ? 1 : 2) : 0;
         t.off = (page * a.cache_stride_p + u.h * a.cache_stride_h + (key & (a.b.page_size() - 1)) * a.cache_stride_s) *
@@ -192,33 +228,33 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                 x.inv = 1.f / left;
             }
         }
-        if (l == 0) consts[j & 1][w] = x;
+        if (l == 0 && own_row == 0) consts[(j + 1) % kSets][own] = x;
     };
     // piece n of the wave's rows of a 16-bit tile of K (tensor 0) or V
     auto transfer = [&](int tensor, desc_t d, int buf, int n) __attribute__((always_inline)) {
         if constexpr (!E8)
             dma16_between(d, lds0 + (tensor ? C::kOffV : 0) + buf * C::kTile + L::base(w * C::kPerWave + n), voff,
-                          n * L::kRows * row_bytes);
+                          (own_row + n * L::kRows) * row_bytes);
     };
     auto desc_of = [&](int tensor, const Group &t) __attribute__((always_inline)) {
         return make_desc((const char *)(tensor ? a.V_cache : a.K_cache) + t.off, t.bytes);
     };
     // e4m3: 16 codes a thread and step
     constexpr int RPW = 64 / C::kChunks;  // rows of a wave's step
-    u32x4 codes[E8 ? C::kPerThread : 1];
+    u32x4 ck[E8 ? C::kPerThread : 1], cv[E8 ? C::kPerThread : 1];
     const uint32_t at8 = l % C::kChunks * 16 < Dr ? l / C::kChunks * row_bytes + l % C::kChunks * 16 : kPast;
-    auto fetch = [&](int tensor, const Group &t) __attribute__((always_inline)) {
+    auto fetch = [&](int tensor, const Group &t, auto &codes) __attribute__((always_inline)) {
         if constexpr (E8) {
             const rsrc_t d = make_rsrc((const char *)(tensor ? a.V_cache : a.K_cache) + t.off, t.bytes);
 #pragma unroll
-            for (int n = 0; n < C::kPerThread; ++n) codes[n] = buf_load16(d, at8, n * RPW * row_bytes);
+            for (int n = 0; n < C::kPerThread; ++n) codes[n] = buf_load16(d, at8, (own_row + n * RPW) * row_bytes);
         }
     };
-    auto convert = [&](int tensor, float by, int buf) __attribute__((always_inline)) {
+    auto convert = [&](int tensor, float by, int buf, const auto &codes) __attribute__((always_inline)) {
         if constexpr (E8) {
 #pragma unroll
             for (int n = 0; n < C::kPerThread; ++n) {
-                const int row = 16 * w + n * RPW + l / C::kChunks, c = l % C::kChunks;
+                const int row = C::kWaveRows * w + n * RPW + l / C::kChunks, c = l % C::kChunks;
                 char *const to = smem + (tensor ? C::kOffV : 0) + buf * C::kTile;
                 *(elem8 *)(to + L::at(row, 2 * c)) = from_e4m3(codes[n].x, codes[n].y, by, by);
                 *(elem8 *)(to + L::at(row, 2 * c + 1)) = from_e4m3(codes[n].z, codes[n].w, by, by);
@@ -245,23 +281,23 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         key0 = t0 * BC;
         key1 = min(t1 * BC, s.len);
         const int T = t1 - t0;
-        // First the 32 keys of sub-tile 0, as the second half of K's "tile -1" and of V's tile 0, and the unit's rows of Q
-        // to the second buffers, in the layout of the tiles: 64 in K's, 64 in V's.
-        Group now = group_of(-1, id_of(-1)), next = group_of(0, id_of(0));  // of sets j, j + 1
-        int ahead = id_of(1);                                               // of set j + 2
-        tell(-1, now);
-        tell(0, next);
-        {
-            const desc_t Kd = desc_of(0, now), Vd = desc_of(1, now);
+        // First the 32 keys of sub-tile 0, as the second half of K's "tile -1" and of V's tile 0, and the unit's rows of Q,
+        // in the layout of the tiles, to the other buffers.
+        const bool active = w * 32 < rows;  // (a wave without rows only fetches)
+        constexpr int A = C::kBufs - 1;  // 16-bit tiles are requested so many ahead of their use
+        Group sets[3] = {group_of(-1, id_of(-1)), group_of(0, id_of(0))};  // of sets j, j + 1, .. j + A
+        int ahead = id_of(1);                                              // of the set behind them
+        tell(-1, sets[0]);
+        tell(0, sets[1]);
+        auto transfer_all = [&](int tensor, const Group &t, int buf) __attribute__((always_inline)) {
+            const desc_t d = desc_of(tensor, t);
 #pragma unroll
-            for (int n = 0; n < C::kPerWave; ++n) {
-                transfer(0, Kd, 0, n);
-                transfer(1, Vd, 0, n);
-            }
-        }
-        fetch(0, now);
-        convert(0, 1.f, 0);
-        fetch(1, now);
+            for (int n = 0; n < C::kPerWave; ++n) transfer(tensor, d, buf, n);
+        };
+        transfer_all(0, sets[0], 0);
+        transfer_all(1, sets[0], 0);
+        fetch(0, sets[0], ck);
+        fetch(1, sets[0], cv);
         {
             constexpr int CPR = D / 8;
 #pragma unroll
@@ -271,15 +307,16 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                 u32x4 x = {0u, 0u, 0u, 0u};
                 if (qr < rows && c * 8 < Dr)
                     x = *(const u32x4 *)(a.Q + (s.first + t) * a.q_stride_t + (u.h * G + q - t * G) * a.q_stride_h + c * 8);
-                *(u32x4 *)(smem + C::kTile + (qr >> 6) * C::kOffV + L::at(qr & 63, c)) = x;
+                *(u32x4 *)(smem + C::area(qr >> 6) + L::at(qr & 63, c)) = x;
             }
         }
-        convert(1, now.v, 0);
+        convert(0, 1.f, 0, ck);
+        convert(1, sets[0].v, 0, cv);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         elem8 qf[KS];
         {
-            const char *Qs = smem + C::kTile + (w >> 1) * C::kOffV + (w & 1) * C::kHalf + k_lane;
+            const char *Qs = smem + C::area(w >> 1) + (w & 1) * C::kHalf + k_lane;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const elem8 *)(Qs + L::step(ks));
         }
@@ -294,13 +331,21 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) sa = mfma32(*(const elem8 *)(smem + C::kHalf + L::step(ks) + k_lane), qf[ks], sa);
         __syncthreads();  // Q and K's "tile -1" are read
-        {
-            const desc_t Kd = desc_of(0, next);
-#pragma unroll
-            for (int n = 0; n < C::kPerWave; ++n) transfer(0, Kd, 0, n);
+        transfer_all(0, sets[1], 0);
+        fetch(0, sets[1], ck);
+        convert(0, 1.f, 0, ck);
+        if constexpr (E8 || A > 1) {
+            sets[2] = group_of(1, ahead);
+            ahead = id_of(2);
+            tell(1, sets[2]);
         }
-        fetch(0, next);
-        convert(0, 1.f, 0);
+        if constexpr (A > 1) {
+            transfer_all(1, sets[1], 1);
+            transfer_all(0, sets[2], 1);
+        }
+        // (e4m3: the codes of the tiles behind, on their way for a whole tile)
+        fetch(1, sets[1], cv);
+        fetch(0, sets[2], ck);
         elem8 pp[2];  // probabilities of the sub-tile before
 #pragma unroll
         for (int i = 0; i < 8; ++i) pp[0][i] = pp[1][i] = (elem)0.f;
@@ -336,7 +381,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             Pair t;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const Const x = consts[j & 1][g + i];
+                const Const x = consts[(j + 1) % kSets][g + i];
                 t.c[i] = E8 ? pin_scalar(x.c) : a.scale_log2e;
                 t.rest[i] = pin_scalar(x.rest);
                 t.inv[i] = E8 ? pin_scalar(x.inv) : 1.f;
@@ -358,10 +403,10 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             for (int p = 0; p < NP; ++p) {
                 if (p + 1 < NP) load(half, p + 1, f[(p + 1) & 1]);
                 else if (half == 0) load(1, 0, f[0]);
-                if (half == 0) {
-                    static_assert(C::kPerWave == NP, "a piece of K and of V a phase");
-                    transfer(0, Kd, fill, p);
-                    transfer(1, Vd, fill, p);
+                if (half == 0 && p % (NP / C::kPerWave) == 0) {
+                    static_assert(NP % C::kPerWave == 0, "pieces divide evenly");
+                    transfer(0, Kd, fill, p / (NP / C::kPerWave));
+                    transfer(1, Vd, fill, p / (NP / C::kPerWave));
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -407,33 +452,51 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                               e[8 * g + 7]);
         };
         Pair behind = pair_of(-1, 2);
-        now = next;
+        int buf = 0;
         for (int j = 0; j < T; ++j) {
-            const int buf = j & 1;
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();  // tiles j are there, and tiles j - 1 are read
+            // tiles j are there (and those behind them on their way), and tiles j - 1 are read
+            wait_vm_and_barrier<E8 ? 63 : (A - 1) * 2 * C::kPerWave>();
+            const int fill = buf + A >= C::kBufs ? buf + A - C::kBufs : buf + A;
             set_bases(buf);
             load(0, 0, f[0]);
             const Pair first = pair_of(j, 0), second = pair_of(j, 2);
-            next = group_of(j + 1, ahead);
-            ahead = id_of(j + 2);
-            Vd = desc_of(1, now);
-            Kd = desc_of(0, next);
-            fetch(1, now);
-            tell(j + 1, next);
             const int kb = key0 + 64 * j;
-            step(kb + 31 > all_see, 0, kb, buf ^ 1, behind, sa, sb);
-            convert(1, now.v, buf ^ 1);
-            fetch(0, next);
-            step(kb + 63 > all_see, 1, kb + 32, buf ^ 1, first, sb, sa);
-            convert(0, 1.f, buf ^ 1);
+            // the tiles A further: set j + A as K's, set j + A - 1 as V's; e4m3: one more, into registers
+            constexpr int F = E8 ? 2 : A;
+            const Group newest = group_of(j + F, ahead);
+            ahead = id_of(j + F + 1);
+            tell(j + F, newest);
+            if constexpr (!E8) {
+                Kd = desc_of(0, newest);
+                Vd = desc_of(1, sets[F]);
+            }
+            if (active) {
+                step(kb + 31 > all_see, 0, kb, fill, behind, sa, sb);
+            } else if constexpr (!E8) {
+#pragma unroll
+                for (int n = 0; n < C::kPerWave; ++n) {
+                    transfer(0, Kd, fill, n);
+                    transfer(1, Vd, fill, n);
+                }
+            }
+            convert(1, sets[1].v, fill, cv);
+            fetch(1, sets[2], cv);
+            if (active) step(kb + 63 > all_see, 1, kb + 32, fill, first, sb, sa);
+            convert(0, 1.f, fill, ck);
+            fetch(0, newest, ck);
             behind = second;
-            now = next;
+            if constexpr (E8 || A > 1) {
+                sets[1] = sets[2];
+                sets[2] = newest;
+            } else {
+                sets[1] = newest;
+            }
+            buf = buf + 1 == C::kBufs ? 0 : buf + 1;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         // the last probabilities' products
-        set_bases(T & 1);
+        set_bases(buf);
 #pragma unroll
         for (int p = 0; p < NS; ++p) {
             load(0, NS + p, f[0]);
@@ -487,20 +550,10 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                 slots.join[me] = PagedJoin{s.first, u.h, u.rt * BR, rows, (int)(last / span.size) - me + 1};
             }
         }
-        todo -= t1 - t0;
-        if (!SPLIT || todo == 0) return;
+        todo -= t1 - t0 + (to_end ? kChunkEnd : 0);
+        if (!SPLIT || todo <= 0) return;
         __syncthreads();  // the rows of O are read: the buffers take the next unit's tiles
-        u.t = 0;
-        if (++u.rt == row_tiles) {
-            u.rt = 0;
-            walk = ChunkWalk(G, BR);
-            if (++u.h == Hkv) {
-                u.h = 0;
-                do set_seq(paged_seq_scalar(a.b, ++u.b)); while (row_tiles == 0);
-            }
-        }
-        u.token = walk.next();
-        u.tiles = chunk_tiles(s, causal, u.token);
+        next_unit();
     }
 }
 

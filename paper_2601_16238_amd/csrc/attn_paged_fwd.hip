@@ -24,10 +24,11 @@ PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, in
     }
     // A batch that may hold long sequences: all of it by the kernel of many rows, also the sequences of one token next
     // to a chunk, which are bound by their keys' way from memory there as well, while the chunk's products run.
-    // (units of 128 rows, at most: of every sequence one that is not full)
-    const int64_t units = (T * G / 128 + std::min(B, T)) * Hkv, tiles = (keys + 63) / 64;
-    p.workers = (int)std::min<int64_t>(p.kernel_d == 256 ? 256 : 512, units * ((tiles + kChunkSpan - 1) / kChunkSpan));
-    p.bytes = paged_span_bytes(p.workers, 128, p.kernel_d);
+    // (units, at most: of every sequence one that is not full)
+    const int unit = chunk_rows(p.kernel_d);
+    const int64_t units = (T * G / unit + std::min(B, T)) * Hkv, tiles = (keys + 63) / 64;
+    p.workers = (int)std::min<int64_t>(p.kernel_d == 64 ? 512 : 256, units * ((tiles + kChunkSpan - 1) / kChunkSpan));
+    p.bytes = paged_span_bytes(p.workers, unit, p.kernel_d);
     return p;
 }
 #endif
