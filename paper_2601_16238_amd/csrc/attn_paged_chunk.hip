@@ -74,7 +74,7 @@ struct ChunkWalk {
 };
 // What the beginning and end of a unit count as, in tiles: its rows come and go while the matrix pipes wait.
 #ifndef CHUNK_END
-#define CHUNK_END 4
+#define CHUNK_END 3
 #endif
 constexpr int kChunkEnd = CHUNK_END;
 __device__ __forceinline__ int chunk_cost(const PagedSeq &s, int G, int max_q, int BR, bool causal)
@@ -268,15 +268,21 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     for (int j = 0; j < 2; ++j)
         v_lane[j] = C::kOffV + L::at(8 * j + 4 * h + ((l & 15) >> 2), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8;
 
+    // x / G for 0 <= x < 2^17: the product is off by less than x / G 2^-22, and x + 1/2 is no nearer to a multiple of G than 1/2
+    const float inv_group = 1.0f / (float)G;
+    auto over_group = [&](int x) { return (int)(((float)x + 0.5f) * inv_group); };
+
     // ---- units
     while (true) {
         const int rows = min(s.n * G - u.rt * BR, BR), t0 = u.t, t1 = min(u.tiles, u.t + todo);
-        const int row = u.rt * BR + w * 32 + r;             // the lane's row of the sequence and head
-        const int tok = row / G, head = u.h * G + row - tok * G;
+        // the unit's first row: new token and query head of the K/V head's; the lane's row
+        const int base_tok = u.rt * BR / G, base_head = u.rt * BR - base_tok * G;
+        const int in_tok = over_group(base_head + w * 32 + r);
+        const int tok = base_tok + in_tok, head = u.h * G + base_head + w * 32 + r - in_tok * G;
         // the last key that it sees
         const int seen = causal ? min(s.len - s.n + tok, s.len - 1) : s.len - 1;
         // ... and the wave's first row (all see that many)
-        const int all_see = causal ? __builtin_amdgcn_readfirstlane(min(s.len - s.n + (u.rt * BR + w * 32) / G, s.len - 1))
+        const int all_see = causal ? __builtin_amdgcn_readfirstlane(min(s.len - s.n + base_tok + over_group(base_head + w * 32), s.len - 1))
                                    : s.len - 1;
         key0 = t0 * BC;
         key1 = min(t1 * BC, s.len);
@@ -299,15 +305,21 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         fetch(0, sets[0], ck);
         fetch(1, sets[0], cv);
         {
-            constexpr int CPR = D / 8;
+            // (all requested before the first is used; rows and columns that do not exist are read elsewhere and dropped)
+            constexpr int CPR = D / 8, N = BR * CPR / C::kThreads;
+            u32x4 x[N];
+            const int c = tid % CPR, col = c * 8 < Dr ? c * 8 : 0;
 #pragma unroll
-            for (int i = 0; i < BR * CPR / C::kThreads; ++i) {
-                const int id = tid + i * C::kThreads, qr = id / CPR, c = id % CPR;
-                const int q = u.rt * BR + qr, t = q / G;
-                u32x4 x = {0u, 0u, 0u, 0u};
-                if (qr < rows && c * 8 < Dr)
-                    x = *(const u32x4 *)(a.Q + (s.first + t) * a.q_stride_t + (u.h * G + q - t * G) * a.q_stride_h + c * 8);
-                *(u32x4 *)(smem + C::area(qr >> 6) + L::at(qr & 63, c)) = x;
+            for (int i = 0; i < N; ++i) {
+                const int qr = min(tid / CPR + i * (C::kThreads / CPR), rows - 1), t = over_group(base_head + qr);
+                x[i] = *(const u32x4 *)(a.Q + (s.first + base_tok + t) * a.q_stride_t +
+                                        (u.h * G + base_head + qr - t * G) * a.q_stride_h + col);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int qr = tid / CPR + i * (C::kThreads / CPR);
+                const u32x4 z = {0u, 0u, 0u, 0u};
+                *(u32x4 *)(smem + C::area(qr >> 6) + L::at(qr & 63, c)) = qr < rows && c * 8 < Dr ? x[i] : z;
             }
         }
         convert(0, 1.f, 0, ck);
@@ -524,9 +536,10 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
 #pragma unroll
             for (int j = 0; j < 32 / RPI; ++j) {
                 const u32x4 v = *(const u32x4 *)(stg + L::at(RPI * j + lr, lc));
-                const int in = w * 32 + RPI * j + lr, q = u.rt * BR + in, t = q / G;
+                const int in = w * 32 + RPI * j + lr, t = over_group(base_head + in);
                 if (in < rows && lc * 8 < Dr)
-                    *(u32x4 *)(a.O + (s.first + t) * a.out_stride_t + (u.h * G + q - t * G) * a.out_stride_h + lc * 8) = v;
+                    *(u32x4 *)(a.O + (s.first + base_tok + t) * a.out_stride_t +
+                               (u.h * G + base_head + in - t * G) * a.out_stride_h + lc * 8) = v;
             }
             if (there && h == 0)
                 a.LSE[(int64_t)(s.first + tok) * a.Hq + head] = lt > 0.f ? (m + fast_log2(lt)) * kLn2 : -INFINITY;
