@@ -230,6 +230,16 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedBatch &a, int heads, 
     return s;
 }
 
+// Global -> LDS transfer as dma16 (attn_device.hpp), of 16 bytes from an address of each lane's.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16_from(const void *p, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 ::"s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(p) : "m0");
+}
+#pragma clang diagnostic pop
+
 // Four e4m3 codes times the power of two of `scale`.
 __device__ __forceinline__ elem4 from_e4m3(uint32_t codes, float scale)
 {

@@ -30,14 +30,15 @@ struct ChunkCfg {
     static constexpr int kHalf = kTile / 2;                   // 32 rows further
     static constexpr int kBufs = D == 128 && !E8 ? 3 : 2;     // of K, and of V
     static constexpr int kOffV = kBufs * kTile;
-    static constexpr int kAreas = kNW / 2;                    // 64 rows of Q each, in the buffers that are free at first
-    static constexpr int kLds = (kAreas > 2 * (kBufs - 1) ? 2 * kBufs + kAreas - 2 * (kBufs - 1) : 2 * kBufs) * kTile;
+    static constexpr int kAreas = kNW / 2;                    // 64 rows of Q each
+    // (and behind everything the rows of O on their way out, 64 bytes of each at a time)
+    static constexpr int kOut = (2 * kBufs + kAreas - 2) * kTile, kOutWave = 32 * 64 + 4 * 16;
+    static constexpr int kLds = kOut + kNW * kOutWave;
     static constexpr int kWaveRows = kBC / kNW;               // of a tile, fetched by a wave
-    // place of rows 64 i .. of Q
+    // place of rows 64 i .. of Q: the last buffers, and behind them
     __device__ static int area(int i)
     {
-        constexpr int kFree = kBufs - 1;  // of K, and of V
-        return i < kFree ? (1 + i) * kTile : i < 2 * kFree ? kOffV + (1 + i - kFree) * kTile : (2 * kBufs + i - 2 * kFree) * kTile;
+        return i == 0 ? (kBufs - 1) * kTile : i == 1 ? kOffV + (kBufs - 1) * kTile : (2 * kBufs + i - 2) * kTile;
     }
     static constexpr int kChunks = D / 16;                    // 16-byte pieces of an e4m3 row
     static constexpr int kPerThread = kBC * kChunks / kThreads;
@@ -47,44 +48,80 @@ struct ChunkCfg {
     static_assert(kPerUnit * kLds <= 160 * 1024, "LDS of a compute unit");
 };
 
-// Units of rows of a sequence: rt has the rows rt BR .. of the sequence's n G.
-__device__ __forceinline__ int chunk_row_tiles(const PagedSeq &s, int G, int max_q, int BR)
+// sum of floor((a i + b) / m) over i = 0 .. n-1, by the steps of Euclid's algorithm on (a, m).
+__device__ __forceinline__ int64_t floor_sum(unsigned n, unsigned m, unsigned a, unsigned b)
 {
-    return s.n > max_q ? 0 : (int)(((unsigned)(s.n * G) + BR - 1) / BR);
-}
-// Tiles of keys that the rows up to the end of new token `token` see (none: one, in which nothing is seen).
-__device__ __forceinline__ int chunk_tiles(const PagedSeq &s, bool causal, int token)
-{
-    const int keys = causal ? min(s.len - s.n + min(token, s.n - 1) + 1, s.len) : s.len;
-    return max((keys + 63) >> 6, 1);
-}
-// Walks over a sequence's units: their last tokens, without a division each.
-struct ChunkWalk {
-    int quot, rem, G, token, left;
-    __device__ ChunkWalk(int G_, int BR) : quot(BR / G_), rem(BR % G_), G(G_), token(-1), left(0) {}
-    // the last token that the next unit has a row of
-    __device__ int next()
-    {
-        // rows so far: (rt + 1) BR = tokens G + left
-        token += quot;
-        left += rem;
-        if (left >= G) { left -= G; ++token; }
-        return left ? token + 1 : token;
+    int64_t sum = 0;
+    while (n) {
+        if (a >= m) {
+            sum += (int64_t)n * (n - 1) / 2 * (a / m);
+            a %= m;
+        }
+        if (b >= m) {
+            sum += (int64_t)n * (b / m);
+            b %= m;
+        }
+        const unsigned most = a * n + b;
+        if (most < m) break;
+        n = most / m;
+        b = most % m;
+        const unsigned t = a;
+        a = m;
+        m = t;
     }
-};
+    return sum;
+}
 // What the beginning and end of a unit count as, in tiles: its rows come and go while the matrix pipes wait.
 #ifndef CHUNK_END
 #define CHUNK_END 3
 #endif
 constexpr int kChunkEnd = CHUNK_END;
-__device__ __forceinline__ int chunk_cost(const PagedSeq &s, int G, int max_q, int BR, bool causal)
-{
-    const int row_tiles = chunk_row_tiles(s, G, max_q, BR);
-    ChunkWalk walk(G, BR);
-    int sum = 0;
-    for (int rt = 0; rt < row_tiles; ++rt) sum += chunk_tiles(s, causal, walk.next()) + kChunkEnd;
-    return sum;
-}
+// The units of a sequence and K/V head, unit rt with the rows rt BR .. of the sequence's n G, and their tiles of 64 keys:
+// those that its last row sees (none: one, in which nothing is seen).  Under a causal mask these are
+//     ceil((len - n + ceil((rt + 1) BR / G)) / 64) = floor((len - n) / 64) + floor(((rt + 1) BR + r G + 64 G - 1) / (64 G)),
+// r = (len - n) mod 64, but for the last unit, which ends with the sequence, and the first `ones`, which see 64 at most.
+struct ChunkUnits {
+    int units, last, q0, ones, len;
+    unsigned m, b, BR;
+    bool causal;
+    __device__ ChunkUnits() {}
+    __device__ ChunkUnits(const PagedSeq &s, int G, int max_q, int BR_, bool causal_) : len(s.len), BR(BR_), causal(causal_)
+    {
+        units = s.n > max_q ? 0 : (int)(((unsigned)(s.n * G) + BR - 1) / BR);
+        last = max((s.len + 63) >> 6, 1);
+        const int before = s.len - s.n;
+        q0 = before >> 6;
+        m = 64u * G;
+        b = BR + (unsigned)(before & 63) * G + m - 1;
+        ones = before >= 64 ? 0 : min((int)((unsigned)(64 - before) * G / BR), units);
+    }
+    __device__ int tiles(int rt) const
+    {
+        if (!causal || rt == units - 1) return last;
+        return rt < ones ? 1 : q0 + (int)((BR * rt + b) / m);
+    }
+    // tiles and ends of the units in front of unit k
+    __device__ int64_t front(int k) const
+    {
+        int64_t sum = (int64_t)k * kChunkEnd;
+        if (!causal) return sum + (int64_t)k * last;
+        const int body = min(k, max(units - 1, 0)), ramp = body - min(body, ones);
+        sum += min(body, ones) + (int64_t)ramp * q0 + floor_sum(ramp, m, BR, b + BR * ones);
+        return k == units && units ? sum + last : sum;
+    }
+    // the unit that position `at` lies in; by a whole wave, 64 candidates at a time
+    __device__ int find(int64_t at) const
+    {
+        int lo = 0, n = units;  // in lo .. lo + n - 1
+        while (n > 1) {
+            const int step = (n + 63) >> 6, k = min(lo + (int)(threadIdx.x & 63) * step, lo + n - 1);
+            const int c = __popcll(__builtin_amdgcn_ballot_w64(front(k) <= at && lo + (int)(threadIdx.x & 63) * step < lo + n)) - 1;
+            n = min(step, lo + n - (lo + c * step));
+            lo += c * step;
+        }
+        return __builtin_amdgcn_readfirstlane(lo);
+    }
+};
 
 constexpr float kChunkOverflow = 1024.0f;  // a lane's sum of a score block above this moves the reference maximum
 constexpr float kChunkMinusHuge = -1.0e30f;
@@ -106,61 +143,54 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     const bool causal = a.causal;
 
     // ---- the span: consecutive units of one XCD, which share K/V heads
-    struct Unit { int b, h, rt, t, tiles, token; };
+    struct Unit { int b, h, rt, t, tiles; };
     PagedSeq s;
-    int row_tiles, todo;
+    ChunkUnits units;
+    int todo;
     Unit u;
-    ChunkWalk walk(G, BR);
     PagedSpan span = {};
     const int me = SPLIT ? xcd_contiguous_order(blockIdx.x, gridDim.x) : blockIdx.x;
+    auto units_of = [&](const PagedSeq &q) { return ChunkUnits(q, G, a.max_q, BR, causal); };
     auto set_seq = [&](const PagedSeq &q) __attribute__((always_inline)) {
         s = q;
-        row_tiles = chunk_row_tiles(q, G, a.max_q, BR);
+        units = units_of(q);
     };
     auto next_unit = [&]() __attribute__((always_inline)) {
         u.t = 0;
-        if (++u.rt == row_tiles) {
+        if (++u.rt == units.units) {
             u.rt = 0;
-            walk = ChunkWalk(G, BR);
             if (++u.h == Hkv) {
                 u.h = 0;
-                do set_seq(paged_seq_scalar(a.b, ++u.b)); while (row_tiles == 0);
+                do set_seq(paged_seq_scalar(a.b, ++u.b)); while (units.units == 0);
             }
         }
-        u.token = walk.next();
-        u.tiles = chunk_tiles(s, causal, u.token);
+        u.tiles = units.tiles(u.rt);
     };
     if constexpr (SPLIT) {
-        span = paged_span<NW>(a.b, Hkv, me, gridDim.x, kChunkSpan, scan,
-                              [&](const PagedSeq &q) { return chunk_cost(q, G, a.max_q, BR, causal); });
+        span = paged_span<NW>(a.b, Hkv, me, gridDim.x, kChunkSpan, scan, [&](const PagedSeq &q) {
+            const ChunkUnits c = units_of(q);
+            return (int)c.front(c.units);
+        });
         todo = span.left;
         if (tid == 0) slots.join[me].pieces = 0;
         if (todo == 0) return;
         u.b = span.b;
         set_seq(span.seq);
         // which head, which unit of it and which of its tiles
-        int cost = 0;
-        for (int rt = 0; rt < row_tiles; ++rt) cost += chunk_tiles(s, causal, walk.next()) + kChunkEnd;
-        int in = (int)(span.begin - span.front);
+        const int cost = __builtin_amdgcn_readfirstlane((int)units.front(units.units));
+        int in = __builtin_amdgcn_readfirstlane((int)(span.begin - span.front));
         u.h = in / cost;
         in -= u.h * cost;
-        walk = ChunkWalk(G, BR);
-        u.rt = 0;
-        while (true) {
-            u.token = walk.next();
-            u.tiles = chunk_tiles(s, causal, u.token);
-            if (in < u.tiles + kChunkEnd) break;
-            in -= u.tiles + kChunkEnd;
-            ++u.rt;
-        }
-        u.t = in;
-        if (in >= u.tiles) {  // the span begins with the end of a unit
-            todo -= u.tiles + kChunkEnd - in;
+        u.rt = units.find(in);
+        u.tiles = units.tiles(u.rt);
+        u.t = in - __builtin_amdgcn_readfirstlane((int)units.front(u.rt));
+        if (u.t >= u.tiles) {  // the span begins with the end of a unit
+            todo -= u.tiles + kChunkEnd - u.t;
             if (todo <= 0) return;
             next_unit();
         }
     } else {
-        // one work-group for each unit: row tiles of a sequence from floor(first G / BR) + b on
+        // one work-group for each unit: those of a sequence from floor(first G / BR) + b on
         const int64_t slot = blockIdx.x / Hkv;
         u.h = blockIdx.x % Hkv;
         int b = -1;
@@ -168,16 +198,14 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             const int bl = min(b0 + l, B - 1);
             const PagedSeq q = paged_seq(a.b, bl);
             const int64_t from = (int64_t)q.first * G / BR + bl;
-            const uint64_t is = __builtin_amdgcn_ballot_w64(b0 + l < B && slot >= from &&
-                                                            slot < from + chunk_row_tiles(q, G, a.max_q, BR));
+            const uint64_t is = __builtin_amdgcn_ballot_w64(b0 + l < B && slot >= from && slot < from + units_of(q).units);
             if (is) b = __builtin_amdgcn_readfirstlane(b0 + __builtin_ctzll(is));
         }
         if (b < 0) return;
         set_seq(paged_seq_scalar(a.b, b));
-        u.rt = __builtin_amdgcn_readfirstlane((int)(slot - ((int64_t)s.first * G / BR + b)));
         u.b = b;
-        for (int rt = 0; rt <= u.rt; ++rt) u.token = walk.next();
-        u.tiles = chunk_tiles(s, causal, u.token);
+        u.rt = __builtin_amdgcn_readfirstlane((int)(slot - ((int64_t)s.first * G / BR + b)));
+        u.tiles = units.tiles(u.rt);
         u.t = 0;
         todo = u.tiles;
     }
@@ -250,11 +278,11 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             for (int n = 0; n < C::kPerThread; ++n) codes[n] = buf_load16(d, at8, (own_row + n * RPW) * row_bytes);
         }
     };
-    auto convert = [&](int tensor, float by, int buf, const auto &codes) __attribute__((always_inline)) {
+    auto convert = [&](int tensor, float by, int buf, const auto &codes, int shift = 0) __attribute__((always_inline)) {
         if constexpr (E8) {
 #pragma unroll
             for (int n = 0; n < C::kPerThread; ++n) {
-                const int row = C::kWaveRows * w + n * RPW + l / C::kChunks, c = l % C::kChunks;
+                const int row = C::kWaveRows * w + n * RPW + l / C::kChunks + shift, c = l % C::kChunks;
                 char *const to = smem + (tensor ? C::kOffV : 0) + buf * C::kTile;
                 *(elem8 *)(to + L::at(row, 2 * c)) = from_e4m3(codes[n].x, codes[n].y, by, by);
                 *(elem8 *)(to + L::at(row, 2 * c + 1)) = from_e4m3(codes[n].z, codes[n].w, by, by);
@@ -272,58 +300,89 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     const float inv_group = 1.0f / (float)G;
     auto over_group = [&](int x) { return (int)(((float)x + 0.5f) * inv_group); };
 
-    // ---- units
-    while (true) {
-        const int rows = min(s.n * G - u.rt * BR, BR), t0 = u.t, t1 = min(u.tiles, u.t + todo);
-        // the unit's first row: new token and query head of the K/V head's; the lane's row
-        const int base_tok = u.rt * BR / G, base_head = u.rt * BR - base_tok * G;
-        const int in_tok = over_group(base_head + w * 32 + r);
-        const int tok = base_tok + in_tok, head = u.h * G + base_head + w * 32 + r - in_tok * G;
-        // the last key that it sees
-        const int seen = causal ? min(s.len - s.n + tok, s.len - 1) : s.len - 1;
-        // ... and the wave's first row (all see that many)
-        const int all_see = causal ? __builtin_amdgcn_readfirstlane(min(s.len - s.n + base_tok + over_group(base_head + w * 32), s.len - 1))
-                                   : s.len - 1;
+    // ---- the beginning of a unit.  Everything that its first tiles need is requested at once, while the unit before it
+    // leaves: the 32 keys of sub-tile 0 of K to the first half of V's tile 0 (which nobody has), that tile's second half, the
+    // tiles 0 (and 1) of K and V, and the wave's rows of Q to the buffers that are free.
+    constexpr int A = C::kBufs - 1;  // 16-bit tiles are requested so many ahead of their use
+    int rows = 0, t0 = 0, t1 = 0, base_tok = 0, base_head = 0;  // rows; tiles; first row: new token, query head of the K/V head's
+    Group sets[3] = {};  // of sets j, j + 1, .. j + A
+    int ahead = -1;      // the page of the set behind them
+    auto begin = [&]() __attribute__((always_inline)) {
+        rows = min(s.n * G - u.rt * BR, BR);
+        t0 = u.t;
+        t1 = min(u.tiles, u.t + todo);
+        base_tok = u.rt * BR / G;
+        base_head = u.rt * BR - base_tok * G;
         key0 = t0 * BC;
         key1 = min(t1 * BC, s.len);
-        const int T = t1 - t0;
-        // First the 32 keys of sub-tile 0, as the second half of K's "tile -1" and of V's tile 0, and the unit's rows of Q,
-        // in the layout of the tiles, to the other buffers.
-        const bool active = w * 32 < rows;  // (a wave without rows only fetches)
-        constexpr int A = C::kBufs - 1;  // 16-bit tiles are requested so many ahead of their use
-        Group sets[3] = {group_of(-1, id_of(-1)), group_of(0, id_of(0))};  // of sets j, j + 1, .. j + A
-        int ahead = id_of(1);                                              // of the set behind them
+        const int id0 = id_of(-1), id1 = id_of(0), id2 = id_of(1);
+        sets[0] = group_of(-1, id0);
+        sets[1] = group_of(0, id1);
         tell(-1, sets[0]);
         tell(0, sets[1]);
+        ahead = id2;
+        if constexpr (E8 || A > 1) {
+            ahead = id_of(2);
+            sets[2] = group_of(1, id2);
+            tell(1, sets[2]);
+        }
         auto transfer_all = [&](int tensor, const Group &t, int buf) __attribute__((always_inline)) {
             const desc_t d = desc_of(tensor, t);
 #pragma unroll
             for (int n = 0; n < C::kPerWave; ++n) transfer(tensor, d, buf, n);
         };
-        transfer_all(0, sets[0], 0);
-        transfer_all(1, sets[0], 0);
-        fetch(0, sets[0], ck);
-        fetch(1, sets[0], cv);
-        {
-            // (all requested before the first is used; rows and columns that do not exist are read elsewhere and dropped)
-            constexpr int CPR = D / 8, N = BR * CPR / C::kThreads;
-            u32x4 x[N];
-            const int c = tid % CPR, col = c * 8 < Dr ? c * 8 : 0;
+        if constexpr (!E8) {
+            if (own >= 2) {
+                const desc_t d = desc_of(0, sets[0]);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int qr = min(tid / CPR + i * (C::kThreads / CPR), rows - 1), t = over_group(base_head + qr);
-                x[i] = *(const u32x4 *)(a.Q + (s.first + base_tok + t) * a.q_stride_t +
-                                        (u.h * G + base_head + qr - t * G) * a.q_stride_h + col);
+                for (int n = 0; n < C::kPerWave; ++n)
+                    dma16_between(d, lds0 + C::kOffV + L::base(w * C::kPerWave + n - C::kPieces / 2), voff,
+                                  (own_row + n * L::kRows) * row_bytes);
+                transfer_all(1, sets[0], 0);
             }
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int qr = tid / CPR + i * (C::kThreads / CPR);
-                const u32x4 z = {0u, 0u, 0u, 0u};
-                *(u32x4 *)(smem + C::area(qr >> 6) + L::at(qr & 63, c)) = qr < rows && c * 8 < Dr ? x[i] : z;
+            transfer_all(0, sets[1], 0);
+            if constexpr (A > 1) {
+                transfer_all(1, sets[1], 1);
+                transfer_all(0, sets[2], 1);
             }
         }
-        convert(0, 1.f, 0, ck);
-        convert(1, sets[0].v, 0, cv);
+        // (rows behind the unit's last are the last again, columns that do not exist column 0, which K's zeros take out)
+#pragma unroll
+        for (int n = 0; n < 32 / L::kRows; ++n) {
+            const int row = min(w * 32 + n * L::kRows + L::lane_row(l), rows - 1), t = over_group(base_head + row);
+            const int c = L::lane_chunk(l) * 8;
+            dma16_from(a.Q + (s.first + base_tok + t) * a.q_stride_t + (u.h * G + base_head + row - t * G) * a.q_stride_h +
+                           (c < Dr ? c : 0),
+                       lds0 + C::area(w >> 1) + L::base((w & 1) * (32 / L::kRows) + n));
+        }
+    };
+    // ... e4m3: what passes through registers
+    auto begin_registers = [&]() __attribute__((always_inline)) {
+        if constexpr (E8) {
+            fetch(0, sets[0], ck);
+            fetch(1, sets[0], cv);
+        }
+    };
+
+    // ---- units
+    begin();
+    begin_registers();
+    while (true) {
+        const int in_tok = over_group(base_head + w * 32 + r);  // of the lane's row
+        // the last key that it sees
+        const int seen = causal ? min(s.len - s.n + base_tok + in_tok, s.len - 1) : s.len - 1;
+        // ... and the wave's first row (all see that many)
+        const int all_see = causal ? __builtin_amdgcn_readfirstlane(min(s.len - s.n + base_tok + over_group(base_head + w * 32), s.len - 1))
+                                   : s.len - 1;
+        const int T = t1 - t0;
+        const bool active = w * 32 < rows;  // (a wave without rows only fetches)
+        if constexpr (E8) {
+            if (own >= 2) {
+                convert(1, 1.f, 0, ck, -32);
+                convert(1, sets[0].v, 0, cv);
+            }
+            fetch(0, sets[1], ck);
+        }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         elem8 qf[KS];
@@ -341,23 +400,13 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sa[i] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sa = mfma32(*(const elem8 *)(smem + C::kHalf + L::step(ks) + k_lane), qf[ks], sa);
-        __syncthreads();  // Q and K's "tile -1" are read
-        transfer_all(0, sets[1], 0);
-        fetch(0, sets[1], ck);
-        convert(0, 1.f, 0, ck);
-        if constexpr (E8 || A > 1) {
-            sets[2] = group_of(1, ahead);
-            ahead = id_of(2);
-            tell(1, sets[2]);
+        for (int ks = 0; ks < KS; ++ks) sa = mfma32(*(const elem8 *)(smem + C::kOffV + L::step(ks) + k_lane), qf[ks], sa);
+        if constexpr (E8) {
+            convert(0, 1.f, 0, ck);
+            // (the codes of the tiles behind, on their way for a whole tile)
+            fetch(1, sets[1], cv);
+            fetch(0, sets[2], ck);
         }
-        if constexpr (A > 1) {
-            transfer_all(1, sets[1], 1);
-            transfer_all(0, sets[2], 1);
-        }
-        // (e4m3: the codes of the tiles behind, on their way for a whole tile)
-        fetch(1, sets[1], cv);
-        fetch(0, sets[2], ck);
         elem8 pp[2];  // probabilities of the sub-tile before
 #pragma unroll
         for (int i = 0; i < 8; ++i) pp[0][i] = pp[1][i] = (elem)0.f;
@@ -516,35 +565,52 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             for (int t = 0; t < 4; ++t)
                 o[(4 * p + t) % DB] = mfma32(f[0][t], pp[(4 * p + t) / DB], o[(4 * p + t) % DB]);
         }
-        __syncthreads();  // all tiles are read: the buffers take the rows of O
+        __syncthreads();  // all tiles are read
 
+        // The next unit's first tiles and rows come while this one's leave.
+        struct { int rows, base_tok, base_head, h, first, row0, tiles, t1; bool from_start, to_end; } e =
+            {rows, base_tok, base_head, u.h, s.first, u.rt * BR, u.tiles, t1, t0 == 0, t1 == u.tiles};
+        todo -= t1 - t0 + (e.to_end ? kChunkEnd : 0);
+        const bool more = SPLIT && todo > 0;
+        if (more) {
+            next_unit();
+            begin();
+        }
         const float lt = xhalf_sum(lsum);
-        const bool from_start = t0 == 0, to_end = t1 == u.tiles;
-        const bool there = w * 32 + r < rows;
-        if (!SPLIT || (from_start && to_end)) {
+        const bool there = w * 32 + r < e.rows;
+        if (!SPLIT || (e.from_start && e.to_end)) {
             const float by = lt > 0.f ? 1.f / lt : 0.f;
-            char *const stg = smem + w * C::kHalf;
+            // 32 columns of the wave's rows at a time, through LDS: 16 bytes a lane, 64 of a row
+            char *const stg = smem + C::kOut + w * C::kOutWave;
+            auto at = [](int row, int chunk) { return row * 64 + row / 8 * 16 + chunk * 16; };
+            elem *out[2];
+            bool store[2];
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
+            for (int j = 0; j < 2; ++j) {
+                const int in = w * 32 + 16 * j + l / 4, t = over_group(e.base_head + in);
+                store[j] = in < e.rows;
+                out[j] = a.O + (e.first + e.base_tok + t) * a.out_stride_t + (e.h * G + e.base_head + in - t * G) * a.out_stride_h +
+                         l % 4 * 8;
+            }
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
-                    *(elem4 *)(stg + L::at(r, 4 * db + g) + 8 * h) =
+                    *(elem4 *)(stg + at(r, g) + 8 * h) =
                         pack4(o[db][4 * g] * by, o[db][4 * g + 1] * by, o[db][4 * g + 2] * by, o[db][4 * g + 3] * by);
-            asm volatile("" ::: "memory");  // a wave's LDS accesses execute in order
-            constexpr int CPR = D / 8, RPI = 64 / CPR;
-            const int lr = l / CPR, lc = l % CPR;
+                asm volatile("" ::: "memory");  // a wave's LDS accesses execute in order
 #pragma unroll
-            for (int j = 0; j < 32 / RPI; ++j) {
-                const u32x4 v = *(const u32x4 *)(stg + L::at(RPI * j + lr, lc));
-                const int in = w * 32 + RPI * j + lr, t = over_group(base_head + in);
-                if (in < rows && lc * 8 < Dr)
-                    *(u32x4 *)(a.O + (s.first + base_tok + t) * a.out_stride_t +
-                               (u.h * G + base_head + in - t * G) * a.out_stride_h + lc * 8) = v;
+                for (int j = 0; j < 2; ++j) {
+                    const u32x4 v = *(const u32x4 *)(stg + at(16 * j + l / 4, l % 4));
+                    if (store[j] && db * 32 + l % 4 * 8 < Dr) *(u32x4 *)(out[j] + db * 32) = v;
+                }
+                asm volatile("" ::: "memory");
             }
             if (there && h == 0)
-                a.LSE[(int64_t)(s.first + tok) * a.Hq + head] = lt > 0.f ? (m + fast_log2(lt)) * kLn2 : -INFINITY;
+                a.LSE[(int64_t)(e.first + e.base_tok + in_tok) * a.Hq + e.h * G + e.base_head + w * 32 + r - in_tok * G] =
+                    lt > 0.f ? (m + fast_log2(lt)) * kLn2 : -INFINITY;
         } else {
-            const int64_t slot = 2 * (int64_t)me + (from_start ? 1 : 0);
+            const int64_t slot = 2 * (int64_t)me + (e.from_start ? 1 : 0);
             if (there) {
                 float *const part = slots.part + (slot * BR + w * 32 + r) * D;
 #pragma unroll
@@ -558,15 +624,13 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                     slots.l[slot * BR + w * 32 + r] = lt;
                 }
             }
-            if (from_start && tid == 0) {
-                const int64_t last = span.begin + span.left - 1 + (u.tiles - t1);
-                slots.join[me] = PagedJoin{s.first, u.h, u.rt * BR, rows, (int)(last / span.size) - me + 1};
+            if (e.from_start && tid == 0) {
+                const int64_t last = span.begin + span.left - 1 + (e.tiles - e.t1);
+                slots.join[me] = PagedJoin{e.first, e.h, e.row0, e.rows, (int)(last / span.size) - me + 1};
             }
         }
-        todo -= t1 - t0 + (to_end ? kChunkEnd : 0);
-        if (!SPLIT || todo <= 0) return;
-        __syncthreads();  // the rows of O are read: the buffers take the next unit's tiles
-        next_unit();
+        if (!more) return;
+        begin_registers();
     }
 }
 
