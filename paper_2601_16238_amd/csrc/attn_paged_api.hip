@@ -89,9 +89,9 @@ int fwd_impl(const void *Q, const void *K_cache, const void *V_cache, const floa
     const int rc = check_paged(p, k_scale != nullptr);
     if (rc != ATTN_OK) return rc;
     if (p->max_q < 1 && p->T > 0) return ATTN_ERR_SHAPE;
-    // (tiles of keys of a sequence and head, over all its rows)
+    // (what the tiles of keys of a sequence and head count, over all its rows)
     const int64_t units = (int64_t)std::min(p->max_q, p->T) * (p->Hq / p->Hkv) / 128 + 1;
-    if (units * ((int64_t)p->table_width * p->page_size / 64 + 8) > std::numeric_limits<int32_t>::max()) return ATTN_ERR_SHAPE;
+    if (units * 2 * ((int64_t)p->table_width * p->page_size / 64 + 8) > std::numeric_limits<int32_t>::max()) return ATTN_ERR_SHAPE;
     if (!std::isfinite(p->scale) || !(p->scale > 0.0f)) return ATTN_ERR_SCALE;
     if (p->T == 0 || p->B == 0) return ATTN_OK;
     if (!Q || !K_cache || !V_cache || !page_table || !q_start || !kv_lens || !O || !LSE) return ATTN_ERR_NULL;

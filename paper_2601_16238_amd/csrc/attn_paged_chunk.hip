@@ -71,17 +71,15 @@ __device__ __forceinline__ int64_t floor_sum(unsigned n, unsigned m, unsigned a,
     }
     return sum;
 }
-// What the beginning and end of a unit count as, in tiles: its rows come and go while the matrix pipes wait.
-#ifndef CHUNK_END
-#define CHUNK_END 3
-#endif
-constexpr int kChunkEnd = CHUNK_END;
+// What spans count: a tile as 2, or as 1 where one or two waves have rows (sequences of few rows next to long ones), and the
+// beginning and end of a unit, where its rows come and go, as 6.
+constexpr int kTileCost = 2, kLightCost = 1, kLightRows = 64, kChunkEnd = 6;
 // The units of a sequence and K/V head, unit rt with the rows rt BR .. of the sequence's n G, and their tiles of 64 keys:
 // those that its last row sees (none: one, in which nothing is seen).  Under a causal mask these are
 //     ceil((len - n + ceil((rt + 1) BR / G)) / 64) = floor((len - n) / 64) + floor(((rt + 1) BR + r G + 64 G - 1) / (64 G)),
 // r = (len - n) mod 64, but for the last unit, which ends with the sequence, and the first `ones`, which see 64 at most.
 struct ChunkUnits {
-    int units, last, q0, ones, len;
+    int units, last, q0, ones, len, cost;  // cost: of a tile
     unsigned m, b, BR;
     bool causal;
     __device__ ChunkUnits() {}
@@ -89,6 +87,7 @@ struct ChunkUnits {
     {
         units = s.n > max_q ? 0 : (int)(((unsigned)(s.n * G) + BR - 1) / BR);
         last = max((s.len + 63) >> 6, 1);
+        cost = s.n * G <= kLightRows ? kLightCost : kTileCost;
         const int before = s.len - s.n;
         q0 = before >> 6;
         m = 64u * G;
@@ -100,11 +99,12 @@ struct ChunkUnits {
         if (!causal || rt == units - 1) return last;
         return rt < ones ? 1 : q0 + (int)((BR * rt + b) / m);
     }
-    // tiles and ends of the units in front of unit k
-    __device__ int64_t front(int k) const
+    // cost of the units in front of unit k
+    __device__ int64_t front(int k) const { return (int64_t)k * kChunkEnd + cost * tiles_in_front(k); }
+    __device__ int64_t tiles_in_front(int k) const
     {
-        int64_t sum = (int64_t)k * kChunkEnd;
-        if (!causal) return sum + (int64_t)k * last;
+        if (!causal) return (int64_t)k * last;
+        int64_t sum = 0;
         const int body = min(k, max(units - 1, 0)), ramp = body - min(body, ones);
         sum += min(body, ones) + (int64_t)ramp * q0 + floor_sum(ramp, m, BR, b + BR * ones);
         return k == units && units ? sum + last : sum;
@@ -143,7 +143,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     const bool causal = a.causal;
 
     // ---- the span: consecutive units of one XCD, which share K/V heads
-    struct Unit { int b, h, rt, t, tiles; };
+    struct Unit { int b, h, rt, t, tiles, at; };  // at: where in the unit's cost the span goes on
     PagedSeq s;
     ChunkUnits units;
     int todo;
@@ -156,7 +156,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         units = units_of(q);
     };
     auto next_unit = [&]() __attribute__((always_inline)) {
-        u.t = 0;
+        u.t = u.at = 0;
         if (++u.rt == units.units) {
             u.rt = 0;
             if (++u.h == Hkv) {
@@ -167,7 +167,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         u.tiles = units.tiles(u.rt);
     };
     if constexpr (SPLIT) {
-        span = paged_span<NW>(a.b, Hkv, me, gridDim.x, kChunkSpan, scan, [&](const PagedSeq &q) {
+        span = paged_span<NW>(a.b, Hkv, me, gridDim.x, kTileCost * kChunkSpan, scan, [&](const PagedSeq &q) {
             const ChunkUnits c = units_of(q);
             return (int)c.front(c.units);
         });
@@ -183,9 +183,13 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         in -= u.h * cost;
         u.rt = units.find(in);
         u.tiles = units.tiles(u.rt);
-        u.t = in - __builtin_amdgcn_readfirstlane((int)units.front(u.rt));
+        // (a tile is the span's in which its cost begins)
+        in -= __builtin_amdgcn_readfirstlane((int)units.front(u.rt));
+        u.at = in;
+        u.t = (in + units.cost - 1) / units.cost;
+        if (u.t < u.tiles && u.t * units.cost >= in + todo) return;
         if (u.t >= u.tiles) {  // the span begins with the end of a unit
-            todo -= u.tiles + kChunkEnd - u.t;
+            todo -= u.tiles * units.cost + kChunkEnd - in;
             if (todo <= 0) return;
             next_unit();
         }
@@ -206,8 +210,8 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         u.b = b;
         u.rt = __builtin_amdgcn_readfirstlane((int)(slot - ((int64_t)s.first * G / BR + b)));
         u.tiles = units.tiles(u.rt);
-        u.t = 0;
-        todo = u.tiles;
+        u.t = u.at = 0;
+        todo = u.tiles * units.cost;
     }
 
     // ---- staging
@@ -310,7 +314,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     auto begin = [&]() __attribute__((always_inline)) {
         rows = min(s.n * G - u.rt * BR, BR);
         t0 = u.t;
-        t1 = min(u.tiles, u.t + todo);
+        t1 = min(u.tiles, (u.at + todo + units.cost - 1) / units.cost);
         base_tok = u.rt * BR / G;
         base_head = u.rt * BR - base_tok * G;
         key0 = t0 * BC;
@@ -568,9 +572,10 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         __syncthreads();  // all tiles are read
 
         // The next unit's first tiles and rows come while this one's leave.
-        struct { int rows, base_tok, base_head, h, first, row0, tiles, t1; bool from_start, to_end; } e =
-            {rows, base_tok, base_head, u.h, s.first, u.rt * BR, u.tiles, t1, t0 == 0, t1 == u.tiles};
-        todo -= t1 - t0 + (e.to_end ? kChunkEnd : 0);
+        struct { int rows, base_tok, base_head, h, first, row0, begins, last; bool from_start, to_end; } e =
+            {rows, base_tok, base_head, u.h, s.first, u.rt * BR, span.left - todo, (u.tiles - 1) * units.cost, t0 == 0,
+             t1 == u.tiles};
+        todo -= e.to_end ? u.tiles * units.cost - u.at + kChunkEnd : todo;
         const bool more = SPLIT && todo > 0;
         if (more) {
             next_unit();
@@ -625,7 +630,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                 }
             }
             if (e.from_start && tid == 0) {
-                const int64_t last = span.begin + span.left - 1 + (e.tiles - e.t1);
+                const int64_t last = span.begin + e.begins + e.last;  // where the unit's last tile begins
                 slots.join[me] = PagedJoin{e.first, e.h, e.row0, e.rows, (int)(last / span.size) - me + 1};
             }
         }
