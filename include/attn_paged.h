@@ -14,7 +14,8 @@
  *   - 16-bit elements of the tensors' type, or
  *   - e4m3 codes (8 bits: OCP float8 with 4 exponent and 3 mantissa bits, largest value 448) where k_scale and v_scale
  *     are given: fp32 [pages][Hkv], contiguous, the value of a code is code * scale[page][head].  The attention takes
- *     any scale that is finite and not negative; attn_paged_append writes powers of two.
+ *     any scale that is 0 or a positive normal number; attn_paged_append writes powers of two.  A code times
+ *     its scale lies in the range of the tensors' type.
  *
  * What device memory holds is not checked on the host.  The kernels stay inside their buffers whatever it is:
  *   - L_b counts as within 0 .. table_width * page_size, row ranges as within 0 .. T;
@@ -39,7 +40,7 @@ typedef struct {
     int32_t D;            /* a multiple of 8 (of 16 with an e4m3 cache), at most 256                        */
     int32_t pages;        /* pages of the cache                                                             */
     int32_t page_size;    /* keys of a page: a power of two, 16 .. 4096                                     */
-    int32_t table_width;  /* entries of a row of the page table; table_width * page_size is an int32        */
+    int32_t table_width;  /* entries of a row of the page table; table_width * page_size is at most 2^30    */
     int32_t table_stride; /* distance of its rows in entries, table_width at least                          */
     int32_t max_q;        /* attention: no sequence has more rows than this (1: decoding).  Rows of a sequence
                              that has more are left as they were.  T is always right.                       */
@@ -66,8 +67,8 @@ void attn_paged_params_contiguous(attn_paged_params_t *p, int32_t T, int32_t B, 
  *     rotated by row p of cos_table, sin_table, fp32 [table_rows][rot/2]:
  *         y_j = x_j c_j - x_{j+rot/2} s_j        y_{j+rot/2} = x_{j+rot/2} c_j + x_j s_j
  *     in fp32; the other columns stay.  rot = 0: K is stored as it comes (tables NULL).
- *   Q, Q_rot: may both be NULL; otherwise the rotated (rot = 0: copied) rows are written to Q_rot, which may be Q (with Q's strides).
- *     Rows at negative positions, or past the page table's, are not written.
+ *   Q, Q_rot: may both be NULL; otherwise the rotated (rot = 0: copied) rows are written to Q_rot, which may be Q
+ *     (with Q's strides).  Rows at negative positions, or past the page table's, are not written.
  *   16-bit cache: the fp32 values, rounded once.  k_scale, v_scale NULL.
  *   e4m3 cache: of each page and head that gets rows, the scale becomes
  *         s = max(old scale if the page has older keys of the sequence, s_new),
@@ -90,6 +91,7 @@ int attn_paged_append_f16(const void *K, const void *V, const void *Q, void *Q_r
 /*
  * Attention of the batch's rows over the cache: O (of Q's type) and LSE, fp32 [T][Hq] contiguous, natural
  * logarithm.  A row that sees no key gets O = 0 and LSE = -infinity.
+ * (T Hq/Hkv / 128 + B) (table_width page_size / 32 + 16), what spreading the work counts with, has to be an int32.
  *   workspace: NULL (every row's keys are worked through by one work-group), or 256-byte aligned and of at least
  *     attn_fwd_paged_workspace_bytes: work over many keys is then spread over the whole chip.  Its contents are not
  *     read before they are written.

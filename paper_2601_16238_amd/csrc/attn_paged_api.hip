@@ -19,7 +19,7 @@ int check_paged(const attn_paged_params_t *p, bool e4m3)
     if (p->D < 8 || p->D > 256 || p->D % (e4m3 ? 16 : 8)) return ATTN_ERR_SHAPE;
     if (p->page_size < 16 || p->page_size > 4096 || (p->page_size & (p->page_size - 1))) return ATTN_ERR_SHAPE;
     if (p->table_stride < p->table_width) return ATTN_ERR_STRIDE;
-    if ((int64_t)p->table_width * p->page_size > lim || (int64_t)p->T * p->Hq > lim ||
+    if ((int64_t)p->table_width * p->page_size > (1 << 30) || (int64_t)p->T * p->Hq > lim ||
         p->Hq > 65535 ||
         // (work-groups of the appending kernel)
         ((int64_t)p->T / p->page_size + 2 * (int64_t)p->B) * p->Hkv * 2 + p->T > lim)
@@ -89,9 +89,9 @@ int fwd_impl(const void *Q, const void *K_cache, const void *V_cache, const floa
     const int rc = check_paged(p, k_scale != nullptr);
     if (rc != ATTN_OK) return rc;
     if (p->max_q < 1 && p->T > 0) return ATTN_ERR_SHAPE;
-    // (what the tiles of keys of a sequence and head count, over all its rows)
-    const int64_t units = (int64_t)std::min(p->max_q, p->T) * (p->Hq / p->Hkv) / 128 + 1;
-    if (units * 2 * ((int64_t)p->table_width * p->page_size / 64 + 8) > std::numeric_limits<int32_t>::max()) return ATTN_ERR_SHAPE;
+    // (what all tiles of keys together count in the spans of the work-groups)
+    const int64_t units = (int64_t)p->T * (p->Hq / p->Hkv) / 128 + p->B, keys = (int64_t)p->table_width * p->page_size;
+    if (units * (keys / 32 + 16) > std::numeric_limits<int32_t>::max()) return ATTN_ERR_SHAPE;
     if (!std::isfinite(p->scale) || !(p->scale > 0.0f)) return ATTN_ERR_SCALE;
     if (p->T == 0 || p->B == 0) return ATTN_OK;
     if (!Q || !K_cache || !V_cache || !page_table || !q_start || !kv_lens || !O || !LSE) return ATTN_ERR_NULL;

@@ -213,7 +213,8 @@ __global__ void __launch_bounds__(THREADS) attn_paged_append8_kernel(const Paged
             u32x4 *at = (u32x4 *)(to + row * a.cache_stride_s + (i - row * (D / 16)) * 16), v = *at;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(v[k], false), y = __builtin_amdgcn_cvt_pk_f32_fp8(v[k], true);
+                const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(v[k], false),
+                            y = __builtin_amdgcn_cvt_pk_f32_fp8(v[k], true);
                 v[k] = to_e4m3(x[0] * ratio, x[1] * ratio, y[0] * ratio, y[1] * ratio);
             }
             *at = v;
@@ -241,8 +242,8 @@ static int launch_append_w(PagedAppendArgs a, hipStream_t st)
     a.nu_magic = (uint32_t)((((uint64_t)1 << 32) + nu - 1) / nu);
     if (!a.k_scale) {
         const int units = ((a.Q_rot ? a.Hq : 0) + 2 * a.Hkv) * nu;
-        hipLaunchKernelGGL(attn_paged_append_kernel<W>, dim3(a.b.T), dim3(units >= 512 ? 512 : (units + 63) / 64 * 64), 0, st,
-                           a);
+        const int threads = units >= 512 ? 512 : (units + 63) / 64 * 64;
+        hipLaunchKernelGGL(attn_paged_append_kernel<W>, dim3(a.b.T), dim3(threads), 0, st, a);
     } else {
         const int slots = (a.b.T >> a.b.page_shift) + 2 * a.b.B;
         const dim3 grid((unsigned)(slots * a.Hkv * 2 + (a.Q_rot ? a.b.T : 0)));

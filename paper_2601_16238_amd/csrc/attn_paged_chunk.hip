@@ -115,7 +115,8 @@ struct ChunkUnits {
         int lo = 0, n = units;  // in lo .. lo + n - 1
         while (n > 1) {
             const int step = (n + 63) >> 6, k = min(lo + (int)(threadIdx.x & 63) * step, lo + n - 1);
-            const int c = __popcll(__builtin_amdgcn_ballot_w64(front(k) <= at && lo + (int)(threadIdx.x & 63) * step < lo + n)) - 1;
+            const bool in_front = front(k) <= at && (int)(threadIdx.x & 63) * step < n;
+            const int c = __popcll(__builtin_amdgcn_ballot_w64(in_front)) - 1;
             n = min(step, lo + n - (lo + c * step));
             lo += c * step;
         }
@@ -220,8 +221,8 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     const uint32_t lds0 = lds_address(smem);
     const uint32_t voff = L::lane_offset(l, row_bytes, Dr, kPast);
     // Set j: the groups 4 j + 2 .. 4 j + 5 of 16 keys each, counted from the unit's first key that the span has; they are
-    // K's tile j and V's tile j + 1.  A wave fetches rows of one group, `own`, and tells the others what its scores are multiplied with, what
-    // is added to the exponents of its probabilities (minus infinity: no page, or behind the last key) and what their
+    // K's tile j and V's tile j + 1.  A wave fetches rows of one group, `own`, and tells the others what its
+    // scores are multiplied with, what is added to the exponents of its probabilities (minus infinity: no page, or behind the last key) and what their
     // sum is multiplied with.
     const int own = w * C::kWaveRows / 16, own_row = w * C::kWaveRows % 16;
     struct Const { float c, rest, inv, unused; };
@@ -300,7 +301,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     for (int j = 0; j < 2; ++j)
         v_lane[j] = C::kOffV + L::at(8 * j + 4 * h + ((l & 15) >> 2), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8;
 
-    // x / G for 0 <= x < 2^17: the product is off by less than x / G 2^-22, and x + 1/2 is no nearer to a multiple of G than 1/2
+    // x / G for 0 <= x < 2^17: the product is off by less than x / G 2^-22, and x + 1/2 is 1/2 away from any multiple of G
     const float inv_group = 1.0f / (float)G;
     auto over_group = [&](int x) { return (int)(((float)x + 0.5f) * inv_group); };
 
@@ -308,7 +309,8 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     // leaves: the 32 keys of sub-tile 0 of K to the first half of V's tile 0 (which nobody has), that tile's second half, the
     // tiles 0 (and 1) of K and V, and the wave's rows of Q to the buffers that are free.
     constexpr int A = C::kBufs - 1;  // 16-bit tiles are requested so many ahead of their use
-    int rows = 0, t0 = 0, t1 = 0, base_tok = 0, base_head = 0;  // rows; tiles; first row: new token, query head of the K/V head's
+    int rows = 0, t0 = 0, t1 = 0;       // rows, tiles
+    int base_tok = 0, base_head = 0;    // the first row: new token, and which query head of the K/V head's
     Group sets[3] = {};  // of sets j, j + 1, .. j + A
     int ahead = -1;      // the page of the set behind them
     auto begin = [&]() __attribute__((always_inline)) {
@@ -376,8 +378,8 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         // the last key that it sees
         const int seen = causal ? min(s.len - s.n + base_tok + in_tok, s.len - 1) : s.len - 1;
         // ... and the wave's first row (all see that many)
-        const int all_see = causal ? __builtin_amdgcn_readfirstlane(min(s.len - s.n + base_tok + over_group(base_head + w * 32), s.len - 1))
-                                   : s.len - 1;
+        const int first_sees = s.len - s.n + base_tok + over_group(base_head + w * 32);
+        const int all_see = causal ? __builtin_amdgcn_readfirstlane(min(first_sees, s.len - 1)) : s.len - 1;
         const int T = t1 - t0;
         const bool active = w * 32 < rows;  // (a wave without rows only fetches)
         if constexpr (E8) {

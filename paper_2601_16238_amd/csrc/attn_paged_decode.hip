@@ -73,7 +73,7 @@ __device__ __forceinline__ int decode_tiles(const PagedSeq &s, int G, int max_ro
 
 // What the end of a unit counts as, in tiles: the waves wait for each other there.  (Without it the spans of short
 // sequences, which end many, were the last to be done.)
-constexpr int kUnitEnd = 1;
+constexpr int kUnitEnd = 2;
 
 // SPLIT: work-groups with spans, partial results in the workspace.  Otherwise one work-group for each sequence and K/V head.
 template <int D, int RB, bool E8, bool SPLIT>
@@ -512,10 +512,12 @@ static int launch_decode_d(const PagedFwdArgs &a, int max_rows, int workers, hip
 int launch_paged_decode(const PagedFwdArgs &a, int D, int max_rows, int workers, hipStream_t st)
 {
     if (a.k_scale)
-        return D == 64 ? launch_decode_d<64, true>(a, max_rows, workers, st) : D == 128 ? launch_decode_d<128, true>(a, max_rows, workers, st)
-                                                                              : launch_decode_d<256, true>(a, max_rows, workers, st);
-    return D == 64 ? launch_decode_d<64, false>(a, max_rows, workers, st) : D == 128 ? launch_decode_d<128, false>(a, max_rows, workers, st)
-                                                                            : launch_decode_d<256, false>(a, max_rows, workers, st);
+        return D == 64 ? launch_decode_d<64, true>(a, max_rows, workers, st)
+             : D == 128 ? launch_decode_d<128, true>(a, max_rows, workers, st)
+                        : launch_decode_d<256, true>(a, max_rows, workers, st);
+    return D == 64 ? launch_decode_d<64, false>(a, max_rows, workers, st)
+         : D == 128 ? launch_decode_d<128, false>(a, max_rows, workers, st)
+                    : launch_decode_d<256, false>(a, max_rows, workers, st);
 }
 
 }  // namespace attn

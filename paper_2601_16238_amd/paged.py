@@ -75,6 +75,6 @@ def attn_fwd_paged(Q, K_cache, V_cache, page_table, q_start, kv_lens, scale, cau
     sees none gets O = 0 and LSE = -inf.  max_q: no sequence has more rows (1 when decoding; a call without it cannot
     know that and also enqueues the kernels for long sequences); rows of one that has more are left as they were, as
     are those behind the last sequence.  `split=False` passes no workspace, which leaves every row's keys to one
-    work-group.  e4m3 caches with their scales (any fp32 scale that is finite and not negative)."""
+    work-group.  e4m3 caches with their scales (any fp32 scale that is 0 or positive and normal)."""
     return _call(marshal().attn_fwd_paged, stream, Q, K_cache, V_cache, page_table, q_start, kv_lens, float(scale),
                  bool(causal), k_scale, v_scale, None if max_q is None else int(max_q), O, LSE, workspace, bool(split))

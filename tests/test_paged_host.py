@@ -53,6 +53,7 @@ BAD = [
     (dict(page_size=8), binding.ATTN_ERR_SHAPE), (dict(page_size=48), binding.ATTN_ERR_SHAPE),
     (dict(page_size=8192), binding.ATTN_ERR_SHAPE), (dict(table_width=0), binding.ATTN_ERR_SHAPE),
     (dict(table_width=1 << 28, table_stride=1 << 28), binding.ATTN_ERR_SHAPE),
+    (dict(table_width=(1 << 26) + 1, table_stride=1 << 27), binding.ATTN_ERR_SHAPE),
     (dict(table_stride=4), binding.ATTN_ERR_STRIDE),
     (dict(T=1 << 30), binding.ATTN_ERR_SHAPE), (dict(Hq=65536 * 2), binding.ATTN_ERR_SHAPE),
     (dict(q_stride_t=516), binding.ATTN_ERR_STRIDE), (dict(q_stride_h=4), binding.ATTN_ERR_STRIDE),
@@ -75,6 +76,9 @@ def test_bad_parameters_of_one_call():
     for s in (0.0, -1.0, float("nan"), float("inf")):
         assert fwd(params(scale=s)) == binding.ATTN_ERR_SCALE
     assert fwd(params(max_q=0)) == binding.ATTN_ERR_SHAPE
+    long = dict(T=1 << 20, max_q=1 << 20, table_width=1 << 20, table_stride=1 << 20)   # rows times keys
+    assert fwd(params(**long)) == binding.ATTN_ERR_SHAPE
+    assert attn.lib().attn_fwd_paged_workspace_bytes(ctypes.byref(params(**long))) > 0
     assert fwd(params(D=72), scales=FAKE) == binding.ATTN_ERR_SHAPE            # e4m3: a multiple of 16
     assert fwd(params(cache_stride_s=72), scales=FAKE) == binding.ATTN_ERR_STRIDE
     for kw in (dict(rot=-8), dict(rot=4), dict(rot=72), dict(table_rows=79)):
