@@ -56,9 +56,9 @@ int launch_paged_chunk(const PagedFwdArgsT<__bf16> &a, int D, int workers, hipSt
 int launch_paged_chunk(const PagedFwdArgsT<_Float16> &a, int D, int workers, hipStream_t st);
 
 // Work in spans: a work-group takes the same number of tiles of keys as every other, from wherever its span begins to
-// wherever it ends.  Of a unit of rows that several have worked on, each leaves a partial result in the workspace: the
-// spans' [2 workers][rows][D] fp32 O relative to a maximum m, in slot 2 w, or 2 w + 1 if it holds the unit's first
-// tile, then m and the sums l, [2 workers][rows] each; and the one that holds the first tile says what is to be joined.
+// wherever it ends.  Of a unit of rows that several have worked on, each leaves a partial result in the workspace: in slot
+// 2 w, or 2 w + 1 if it holds the unit's first tile, rows x D fp32 of O relative to a maximum m, in the kernel's own order,
+// then m and the sums l, [2 workers][rows] each; and the one that holds the first tile says what is to be joined.
 struct PagedJoin {
     int first, head, row0, rows;  // packed row and K/V head of the unit; its rows are row0 .. row0+rows-1 of their grid
     int pieces;                   // workers w, w+1, ..; 0: nothing
@@ -162,6 +162,7 @@ struct PagedSpan {
     int64_t begin, front, size;
     int left, b;  // tiles of the span (0: none)
     PagedSeq seq;
+    int tiles;    // of sequence b
 };
 __device__ __forceinline__ int64_t div_up(int64_t x, int y)
 {
@@ -196,6 +197,7 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedBatch &a, int heads, 
         s.seq.first = __builtin_amdgcn_readlane(q.first, s.b);
         s.seq.n = __builtin_amdgcn_readlane(q.n, s.b);
         s.seq.len = __builtin_amdgcn_readlane(q.len, s.b);
+        s.tiles = __builtin_amdgcn_readlane(mine, s.b);
         return s;
     }
     int64_t total = 0;
@@ -223,6 +225,7 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedBatch &a, int heads, 
             s.b = __builtin_amdgcn_readfirstlane(lds[0]);
             s.front = (s.front + __builtin_amdgcn_readfirstlane(lds[1])) * heads;
             s.seq = paged_seq_scalar(a, s.b);
+            s.tiles = __builtin_amdgcn_readfirstlane(tiles(s.seq));
             return s;
         }
         s.front += all;
@@ -261,80 +264,6 @@ __device__ __forceinline__ float scale_rest(float scale)
 {
     const uint32_t u = __float_as_uint(scale);
     return u ? __uint_as_float((u & 0x7fffffu) | 0x3f800000u) : 0.f;
-}
-
-// The partial results of the units that worker blockIdx.x has the first tile of, joined.  A work-group has kRows rows (grid
-// y), 256 / kRows threads each: D / 4 columns of four, and PAR groups of them that share the pieces.  64 pieces at a
-// time: their maxima and sums come through LDS, so that no load waits for another but the record's.
-template <int D, int PAR>
-__global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedFwdArgs a, const PagedSlots<elem> s, const int R)
-{
-    constexpr int kCols = D / 4, kRows = 256 / kCols / PAR, kPieces = 64;
-    __shared__ float ms[PAR > 1 ? 1 : kPieces][kRows], ls[PAR > 1 ? 1 : kPieces][kRows];
-    __shared__ f32x4 sum[PAR > 1 ? PAR : 1][PAR > 1 ? kCols : 1];
-    static_assert(PAR == 1 || kRows == 1, "one row, or one thread for all pieces");
-    const PagedJoin j = s.join[blockIdx.x];
-    const int tid = threadIdx.x, l = tid & 63, c = tid % kCols, p = PAR > 1 ? tid / kCols : 0, rr = PAR > 1 ? 0 : tid / kCols;
-    const int r0 = blockIdx.y * kRows, r = r0 + rr;
-    if (j.pieces == 0 || r0 >= j.rows) return;
-    auto at = [&](int i, int row) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0)) * R + row; };
-    const bool mine = r < j.rows && 4 * c < a.Dr;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float top = kJoinMinusHuge, all = 0.f;
-    for (int i0 = 0; i0 < j.pieces; i0 += kPieces) {
-        const int n = min(j.pieces - i0, kPieces);
-        float to = top, weight = 0.f, sums = 0.f;
-        if constexpr (PAR > 1) {
-            // one row: a piece a lane, in every wave
-            const bool is = l < n;
-            const float m = is ? s.m[at(i0 + l, r0)] : kJoinMinusHuge, sum_l = is ? s.l[at(i0 + l, r0)] : 0.f;
-            to = fmaxf(to, m);
-#pragma unroll
-            for (int d = 32; d; d /= 2) to = fmaxf(to, __shfl_xor(to, d));
-            weight = fast_exp2(m - to);
-            sums = sum_l * weight;
-#pragma unroll
-            for (int d = 32; d; d /= 2) sums += __shfl_xor(sums, d);
-        } else {
-            if (i0) __syncthreads();
-            for (int k = tid; k < n * kRows; k += 256) {
-                const int i = k / kRows, row = k % kRows;
-                const bool is = r0 + row < j.rows;
-                ms[i][row] = is ? s.m[at(i0 + i, r0 + row)] : 0.f;
-                ls[i][row] = is ? s.l[at(i0 + i, r0 + row)] : 0.f;
-            }
-            __syncthreads();
-#pragma unroll 4
-            for (int i = 0; i < n; ++i) to = fmaxf(to, ms[i][rr]);
-#pragma unroll 4
-            for (int i = 0; i < n; ++i) sums += ls[i][rr] * fast_exp2(ms[i][rr] - to);
-        }
-        const float keep = fast_exp2(top - to);
-        x *= keep;
-        all = all * keep + sums;
-        top = to;
-        // (the first piece lies in its worker's other slot)
-        const float *const part = s.part + at(i0, r) * D + 4 * c;
-        const int64_t step = 2 * (int64_t)R * D, back = i0 == 0 ? (int64_t)R * D : 0;
-#pragma unroll 4
-        for (int i = 0; i < n; i += PAR) {
-            const int k = i + p;
-            const float by = PAR > 1 ? __shfl(weight, k & 63) : fast_exp2(ms[PAR > 1 ? 0 : k][rr] - to);
-            if (k < n && mine) x += *(const f32x4 *)(part + k * step - (k ? back : 0)) * by;
-        }
-    }
-    if constexpr (PAR > 1) {
-        sum[p][c] = x;
-        __syncthreads();
-        if (p) return;
-#pragma unroll
-        for (int i = 1; i < PAR; ++i) x += sum[i][c];
-    }
-    if (!mine) return;
-    const float inv = all > 0.f ? 1.f / all : 0.f;
-    const int G = a.Hq / a.Hkv, row = j.row0 + r, t = j.first + row / G, hq = j.head * G + row % G;
-    *(elem4 *)(a.O + t * a.out_stride_t + hq * a.out_stride_h + 4 * c) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-    if (c == 0) a.LSE[(int64_t)t * a.Hq + hq] = all > 0.f ? (top + fast_log2(all)) * kLn2 : -INFINITY;
 }
 
 }  // namespace attn

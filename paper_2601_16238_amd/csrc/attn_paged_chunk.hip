@@ -109,14 +109,16 @@ struct ChunkUnits {
         sum += min(body, ones) + (int64_t)ramp * q0 + floor_sum(ramp, m, BR, b + BR * ones);
         return k == units && units ? sum + last : sum;
     }
-    // the unit that position `at` lies in; by a whole wave, 64 candidates at a time
-    __device__ int find(int64_t at) const
+    // the unit that position `at` lies in, and what lies in front of it; by a whole wave, 64 candidates at a time
+    __device__ int find(int at, int &in_front_of_it) const
     {
         int lo = 0, n = units;  // in lo .. lo + n - 1
+        in_front_of_it = 0;
         while (n > 1) {
             const int step = (n + 63) >> 6, k = min(lo + (int)(threadIdx.x & 63) * step, lo + n - 1);
-            const bool in_front = front(k) <= at && (int)(threadIdx.x & 63) * step < n;
-            const int c = __popcll(__builtin_amdgcn_ballot_w64(in_front)) - 1;
+            const int f = (int)front(k);
+            const int c = __popcll(__builtin_amdgcn_ballot_w64(f <= at && (int)(threadIdx.x & 63) * step < n)) - 1;
+            in_front_of_it = __builtin_amdgcn_readlane(f, c);
             n = min(step, lo + n - (lo + c * step));
             lo += c * step;
         }
@@ -144,50 +146,54 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     const bool causal = a.causal;
 
     // ---- the span: consecutive units of one XCD, which share K/V heads
-    struct Unit { int b, h, rt, t, tiles, at; };  // at: where in the unit's cost the span goes on
+    struct Unit { int b, h, rt, t, tiles, cost, at; };  // cost of a tile; at: where in the unit's cost the span goes on
     PagedSeq s;
-    ChunkUnits units;
     int todo;
     Unit u;
-    PagedSpan span = {};
+    int64_t begin_at = 0, size = 0;  // of the span
+    int left = 0;
     const int me = SPLIT ? xcd_contiguous_order(blockIdx.x, gridDim.x) : blockIdx.x;
     auto units_of = [&](const PagedSeq &q) { return ChunkUnits(q, G, a.max_q, BR, causal); };
-    auto set_seq = [&](const PagedSeq &q) __attribute__((always_inline)) {
-        s = q;
-        units = units_of(q);
-    };
     auto next_unit = [&]() __attribute__((always_inline)) {
+        // (what the sequence's units are is found again rather than kept: the scalar registers are few)
+        ChunkUnits units = units_of(s);
         u.t = u.at = 0;
         if (++u.rt == units.units) {
             u.rt = 0;
             if (++u.h == Hkv) {
                 u.h = 0;
-                do set_seq(paged_seq_scalar(a.b, ++u.b)); while (units.units == 0);
+                do units = units_of(s = paged_seq_scalar(a.b, ++u.b)); while (units.units == 0);
             }
         }
         u.tiles = units.tiles(u.rt);
+        u.cost = units.cost;
     };
     if constexpr (SPLIT) {
-        span = paged_span<NW>(a.b, Hkv, me, gridDim.x, kTileCost * kChunkSpan, scan, [&](const PagedSeq &q) {
+        const PagedSpan span = paged_span<NW>(a.b, Hkv, me, gridDim.x, kTileCost * kChunkSpan, scan, [&](const PagedSeq &q) {
             const ChunkUnits c = units_of(q);
             return (int)c.front(c.units);
         });
-        todo = span.left;
+        begin_at = span.begin;
+        size = span.size;
+        todo = left = span.left;
         if (tid == 0) slots.join[me].pieces = 0;
         if (todo == 0) return;
         u.b = span.b;
-        set_seq(span.seq);
+        s = span.seq;
+        const ChunkUnits units = units_of(s);
         // which head, which unit of it and which of its tiles
-        const int cost = __builtin_amdgcn_readfirstlane((int)units.front(units.units));
+        const int cost = span.tiles;
         int in = __builtin_amdgcn_readfirstlane((int)(span.begin - span.front));
         u.h = in / cost;
         in -= u.h * cost;
-        u.rt = units.find(in);
+        int front;
+        u.rt = units.find(in, front);
         u.tiles = units.tiles(u.rt);
+        u.cost = units.cost;
         // (a tile is the span's in which its cost begins)
-        in -= __builtin_amdgcn_readfirstlane((int)units.front(u.rt));
+        in -= front;
         u.at = in;
-        u.t = (in + units.cost - 1) / units.cost;
+        u.t = (in + units.cost - 1) >> (units.cost - 1);  // (the cost is 1 or 2)
         if (u.t < u.tiles && u.t * units.cost >= in + todo) return;
         if (u.t >= u.tiles) {  // the span begins with the end of a unit
             todo -= u.tiles * units.cost + kChunkEnd - in;
@@ -207,10 +213,12 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             if (is) b = __builtin_amdgcn_readfirstlane(b0 + __builtin_ctzll(is));
         }
         if (b < 0) return;
-        set_seq(paged_seq_scalar(a.b, b));
+        s = paged_seq_scalar(a.b, b);
+        const ChunkUnits units = units_of(s);
         u.b = b;
         u.rt = __builtin_amdgcn_readfirstlane((int)(slot - ((int64_t)s.first * G / BR + b)));
         u.tiles = units.tiles(u.rt);
+        u.cost = units.cost;
         u.t = u.at = 0;
         todo = u.tiles * units.cost;
     }
@@ -316,7 +324,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     auto begin = [&]() __attribute__((always_inline)) {
         rows = min(s.n * G - u.rt * BR, BR);
         t0 = u.t;
-        t1 = min(u.tiles, (u.at + todo + units.cost - 1) / units.cost);
+        t1 = min(u.tiles, (u.at + todo + u.cost - 1) >> (u.cost - 1));
         base_tok = u.rt * BR / G;
         base_head = u.rt * BR - base_tok * G;
         key0 = t0 * BC;
@@ -575,9 +583,9 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
 
         // The next unit's first tiles and rows come while this one's leave.
         struct { int rows, base_tok, base_head, h, first, row0, begins, last; bool from_start, to_end; } e =
-            {rows, base_tok, base_head, u.h, s.first, u.rt * BR, span.left - todo, (u.tiles - 1) * units.cost, t0 == 0,
+            {rows, base_tok, base_head, u.h, s.first, u.rt * BR, left - todo, (u.tiles - 1) * u.cost, t0 == 0,
              t1 == u.tiles};
-        todo -= e.to_end ? u.tiles * units.cost - u.at + kChunkEnd : todo;
+        todo -= e.to_end ? u.tiles * u.cost - u.at + kChunkEnd : todo;
         const bool more = SPLIT && todo > 0;
         if (more) {
             next_unit();
@@ -618,13 +626,14 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                     lt > 0.f ? (m + fast_log2(lt)) * kLn2 : -INFINITY;
         } else {
             const int64_t slot = 2 * (int64_t)me + (e.from_start ? 1 : 0);
-            if (there) {
-                float *const part = slots.part + (slot * BR + w * 32 + r) * D;
+            if (w * 32 < e.rows) {
+                // as the accumulators lie: every store of a wave is 1 KB
+                float *const part = slots.part + slot * BR * D + w * 32 * D + l * 4;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
-                        *(f32x4 *)(part + 32 * db + 8 * g + 4 * h) =
+                        *(f32x4 *)(part + (4 * db + g) * 256) =
                             f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
                 if (h == 0) {
                     slots.m[slot * BR + w * 32 + r] = m;
@@ -632,13 +641,69 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
                 }
             }
             if (e.from_start && tid == 0) {
-                const int64_t last = span.begin + e.begins + e.last;  // where the unit's last tile begins
-                slots.join[me] = PagedJoin{e.first, e.h, e.row0, e.rows, (int)(last / span.size) - me + 1};
+                const int64_t last = begin_at + e.begins + e.last;  // where the unit's last tile begins
+                slots.join[me] = PagedJoin{e.first, e.h, e.row0, e.rows, (int)(last / size) - me + 1};
             }
         }
         if (!more) return;
         begin_registers();
     }
+}
+
+// The partial results of the units that worker blockIdx.x has the first tile of, joined: a work-group has 32 rows and 32
+// columns (grid y), a thread four columns of a row in all pieces, eight of them at a time and with no load that waits for
+// another but the record's.
+template <int D>
+__global__ void __launch_bounds__(256) attn_paged_join_rows_kernel(const PagedFwdArgs a, const PagedSlots<elem> s)
+{
+    constexpr int DB = D / 32, R = chunk_rows(D), kPieces = 8;
+    __shared__ __attribute__((aligned(16))) elem out[32][40];
+    const PagedJoin j = s.join[blockIdx.x];
+    const int tid = threadIdx.x, r = tid & 31, g = tid >> 6, h = tid >> 5 & 1, w = blockIdx.y / DB, db = blockIdx.y % DB;
+    if (j.pieces == 0 || w * 32 >= j.rows) return;
+    const int row = w * 32 + r;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float top = kJoinMinusHuge, all = 0.f;
+    for (int i0 = 0; i0 < j.pieces; i0 += kPieces) {
+        float m[kPieces], l[kPieces];
+        f32x4 y[kPieces];
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            // (behind the last piece: the last again)
+            const int i = min(i0 + k, j.pieces - 1);
+            const int64_t slot = 2 * (int64_t)(blockIdx.x + i) + (i == 0);
+            m[k] = s.m[slot * R + row];
+            l[k] = s.l[slot * R + row];
+            y[k] = *(const f32x4 *)(s.part + slot * R * D + w * 32 * D + (4 * db + g) * 256 + (tid & 63) * 4);
+        }
+        float to = top;
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) to = fmaxf(to, m[k]);
+        const float keep = fast_exp2(top - to);
+        x *= keep;
+        all *= keep;
+        top = to;
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            const float by = i0 + k < j.pieces ? fast_exp2(m[k] - to) : 0.f;
+            x += y[k] * by;
+            all += l[k] * by;
+        }
+    }
+    const float inv = all > 0.f ? 1.f / all : 0.f;
+    *(elem4 *)&out[r][8 * g + 4 * h] = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    const int G = a.Hq / a.Hkv;
+    if (db == 0 && tid < 32 && row < j.rows) {
+        const int q = j.row0 + row, t = q / G;
+        a.LSE[(int64_t)(j.first + t) * a.Hq + j.head * G + q - t * G] = all > 0.f ? (top + fast_log2(all)) * kLn2 : -INFINITY;
+    }
+    __syncthreads();
+    // 16 bytes a lane, 64 of a row
+    const int in = w * 32 + tid / 4, col = 32 * db + tid % 4 * 8;
+    if (tid >= 128 || in >= j.rows || col >= a.Dr) return;
+    const int q = j.row0 + in, t = q / G;
+    *(u32x4 *)(a.O + (j.first + t) * a.out_stride_t + (j.head * G + q - t * G) * a.out_stride_h + col) =
+        *(const u32x4 *)&out[tid / 4][tid % 4 * 8];
 }
 
 template <int D, bool E8>
@@ -655,8 +720,7 @@ static int launch_chunk_t(const PagedFwdArgs &a, int workers, hipStream_t st)
                            C::kLds, st, a, slots);
     } else {
         hipLaunchKernelGGL((attn_paged_chunk_kernel<D, E8, true>), dim3(workers), dim3(C::kThreads), C::kLds, st, a, slots);
-        hipLaunchKernelGGL((attn_paged_join_kernel<D, 1>), dim3(workers, C::kBR * D / 1024), dim3(256), 0, st, a, slots,
-                           C::kBR);
+        hipLaunchKernelGGL(attn_paged_join_rows_kernel<D>, dim3(workers, C::kBR / 32 * (D / 32)), dim3(256), 0, st, a, slots);
     }
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }

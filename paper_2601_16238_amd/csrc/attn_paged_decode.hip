@@ -481,6 +481,55 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
     }
 }
 
+// The partial results of the units that worker blockIdx.x has the first tile of, joined.  A work-group has one row (grid y),
+// PAR = 1024 / D groups of D / 4 threads that share the pieces, 64 at a time: a piece's maximum and sum in a lane.
+template <int D>
+__global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedFwdArgs a, const PagedSlots<elem> s, const int R)
+{
+    constexpr int kCols = D / 4, PAR = 256 / kCols;
+    __shared__ f32x4 sum[PAR][kCols];
+    const PagedJoin j = s.join[blockIdx.x];
+    const int tid = threadIdx.x, l = tid & 63, c = tid % kCols, p = tid / kCols, r = blockIdx.y;
+    if (j.pieces == 0 || r >= j.rows) return;
+    auto at = [&](int i) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0)) * R + r; };
+    const bool mine = 4 * c < a.Dr;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float top = kJoinMinusHuge, all = 0.f;
+    for (int i0 = 0; i0 < j.pieces; i0 += 64) {
+        const int n = min(j.pieces - i0, 64);
+        const bool is = l < n;
+        const float m = is ? s.m[at(i0 + l)] : kJoinMinusHuge, sum_l = is ? s.l[at(i0 + l)] : 0.f;
+        float to = fmaxf(top, m);
+#pragma unroll
+        for (int d = 32; d; d /= 2) to = fmaxf(to, __shfl_xor(to, d));
+        const float weight = fast_exp2(m - to), keep = fast_exp2(top - to);
+        float sums = sum_l * weight;
+#pragma unroll
+        for (int d = 32; d; d /= 2) sums += __shfl_xor(sums, d);
+        x *= keep;
+        all = all * keep + sums;
+        top = to;
+        // (the first piece lies in its worker's other slot)
+        const float *const part = s.part + at(i0) * D + 4 * c;
+        const int64_t step = 2 * (int64_t)R * D, back = i0 == 0 ? (int64_t)R * D : 0;
+#pragma unroll 4
+        for (int i = 0; i < n; i += PAR) {
+            const int k = i + p;
+            const float by = __shfl(weight, k & 63);
+            if (k < n && mine) x += *(const f32x4 *)(part + k * step - (k ? back : 0)) * by;
+        }
+    }
+    sum[p][c] = x;
+    __syncthreads();
+    if (p || !mine) return;
+#pragma unroll
+    for (int i = 1; i < PAR; ++i) x += sum[i][c];
+    const float inv = all > 0.f ? 1.f / all : 0.f;
+    const int G = a.Hq / a.Hkv, t = j.first + r / G, hq = j.head * G + r % G;
+    *(elem4 *)(a.O + t * a.out_stride_t + hq * a.out_stride_h + 4 * c) = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    if (c == 0) a.LSE[(int64_t)t * a.Hq + hq] = all > 0.f ? (top + fast_log2(all)) * kLn2 : -INFINITY;
+}
+
 template <int D, int RB, bool E8>
 static int launch_decode_t(const PagedFwdArgs &a, int max_rows, int workers, hipStream_t st)
 {
@@ -494,7 +543,7 @@ static int launch_decode_t(const PagedFwdArgs &a, int max_rows, int workers, hip
     } else {
         hipLaunchKernelGGL((attn_paged_decode_kernel<D, RB, E8, true>), dim3(workers), dim3(C::kThreads), C::kLds, st, a,
                            max_rows);
-        hipLaunchKernelGGL((attn_paged_join_kernel<D, 1024 / D>), dim3(workers, max_rows), dim3(256), 0, st, a,
+        hipLaunchKernelGGL(attn_paged_join_kernel<D>, dim3(workers, max_rows), dim3(256), 0, st, a,
                            PagedSlots<elem>(a.workspace, workers, 16 * RB, D), 16 * RB);
     }
     return hipGetLastError() == hipSuccess ? 0 : -1;
