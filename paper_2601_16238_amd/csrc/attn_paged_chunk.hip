@@ -240,8 +240,13 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     auto key_of = [&](int j, int g) { return key0 + 64 * j + 32 + 16 * g; };
     auto id_of = [&](int j) __attribute__((always_inline)) {
         const int key = key_of(j, own);
-        return key >= key0 && key < key1 ? scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride +
-                                                       (key >> a.b.page_shift)) : -1;
+        if constexpr (!E8)
+            return key >= key0 && key < key1 ? scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride +
+                                                           (key >> a.b.page_shift)) : -1;
+        // (loads without branches, here and of the scales, of what is there in any case)
+        const int at = max(min(key, s.len - 1), 0) >> a.b.page_shift;
+        const int id = scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride + at);
+        return key >= key0 && key < key1 ? id : -1;
     };
     // the wave's group: offset of its first row in the cache, bytes that exist of it, and its scales
     struct Group { int64_t off; uint32_t bytes; float k, v; };
@@ -253,8 +258,10 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         t.off = (page * a.cache_stride_p + u.h * a.cache_stride_h + (key & (a.b.page_size() - 1)) * a.cache_stride_s) *
                 (E8 ? 1 : 2);
         if constexpr (E8) {
-            t.k = is ? scalar_load(a.k_scale + (int64_t)page * Hkv + u.h) : 1.f;
-            t.v = is ? scalar_load(a.v_scale + (int64_t)page * Hkv + u.h) : 1.f;
+            const float k = scalar_load(a.k_scale + (int64_t)page * Hkv + u.h),
+                        v = scalar_load(a.v_scale + (int64_t)page * Hkv + u.h);
+            t.k = is ? k : 1.f;
+            t.v = is ? v : 1.f;
         }
         return t;
     };
@@ -320,7 +327,9 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     int rows = 0, t0 = 0, t1 = 0;       // rows, tiles
     int base_tok = 0, base_head = 0;    // the first row: new token, and which query head of the K/V head's
     Group sets[3] = {};  // of sets j, j + 1, .. j + A
-    int ahead = -1;      // the page of the set behind them
+    constexpr int F = E8 ? 2 : A;  // sets in use ahead of tile j's; e4m3: one more, in registers
+    Group following = {};          // e4m3: set j + F
+    int ahead = -1;                // the page of the set behind them
     auto begin = [&]() __attribute__((always_inline)) {
         rows = min(s.n * G - u.rt * BR, BR);
         t0 = u.t;
@@ -329,17 +338,15 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
         base_head = u.rt * BR - base_tok * G;
         key0 = t0 * BC;
         key1 = min(t1 * BC, s.len);
-        const int id0 = id_of(-1), id1 = id_of(0), id2 = id_of(1);
+        const int id0 = id_of(-1), id1 = id_of(0), id2 = id_of(1), id3 = F > 1 ? id_of(2) : id2;
+        ahead = E8 ? id_of(F + 1) : id3;
         sets[0] = group_of(-1, id0);
         sets[1] = group_of(0, id1);
+        if constexpr (F > 1) sets[2] = group_of(1, id2);
+        if constexpr (E8) following = group_of(F, id3);
         tell(-1, sets[0]);
         tell(0, sets[1]);
-        ahead = id2;
-        if constexpr (E8 || A > 1) {
-            ahead = id_of(2);
-            sets[2] = group_of(1, id2);
-            tell(1, sets[2]);
-        }
+        if constexpr (F > 1) tell(1, sets[2]);
         auto transfer_all = [&](int tensor, const Group &t, int buf) __attribute__((always_inline)) {
             const desc_t d = desc_of(tensor, t);
 #pragma unroll
@@ -537,9 +544,8 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             const Pair first = pair_of(j, 0), second = pair_of(j, 2);
             const int kb = key0 + 64 * j;
             // the tiles A further: set j + A as K's, set j + A - 1 as V's; e4m3: one more, into registers
-            constexpr int F = E8 ? 2 : A;
-            const Group newest = group_of(j + F, ahead);
-            ahead = id_of(j + F + 1);
+            const Group newest = E8 ? following : group_of(j + F, ahead);
+            if constexpr (!E8) ahead = id_of(j + F + 1);
             tell(j + F, newest);
             if constexpr (!E8) {
                 Kd = desc_of(0, newest);
@@ -559,8 +565,13 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             if (active) step(kb + 63 > all_see, 1, kb + 32, fill, first, sb, sa);
             convert(0, 1.f, fill, ck);
             fetch(0, newest, ck);
+            // (scalar loads just before the barrier, which waits for them: inside a step, every wait for LDS would)
+            if constexpr (E8) {
+                following = group_of(j + F + 1, ahead);
+                ahead = id_of(j + F + 2);
+            }
             behind = second;
-            if constexpr (E8 || A > 1) {
+            if constexpr (F > 1) {
                 sets[1] = sets[2];
                 sets[2] = newest;
             } else {

@@ -168,8 +168,10 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
             const int key = u.t * TK + w * 32 + 16 * hf;
-            p.id[hf] = key < u.len ? scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride +
-                                                 (key >> a.b.page_shift)) : -1;
+            // (without a branch: there is an entry in any case)
+            const int at = max(min(key, u.len - 1), 0) >> a.b.page_shift;
+            const int id = scalar_load(a.b.page_table + (int64_t)u.b * a.b.table_stride + at);
+            p.id[hf] = key < u.len ? id : -1;
         }
         return p;
     };
@@ -187,8 +189,10 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
             const desc_t Kd = make_desc((const char *)a.K_cache + off, bytes),
                          Vd = make_desc((const char *)a.V_cache + off, bytes);
             if constexpr (E8) {
-                sc.k[hf] = is ? scalar_load(a.k_scale + (int64_t)id * Hkv + u.h) : 1.f;
-                sc.v[hf] = is ? scalar_load(a.v_scale + (int64_t)id * Hkv + u.h) : 1.f;
+                const float k = scalar_load(a.k_scale + (int64_t)id * Hkv + u.h),
+                            v = scalar_load(a.v_scale + (int64_t)id * Hkv + u.h);
+                sc.k[hf] = is ? k : 1.f;
+                sc.v[hf] = is ? v : 1.f;
             }
 #pragma unroll
             for (int n = 0; n < KP / 2; ++n) {
