@@ -485,17 +485,17 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
     }
 }
 
-// The partial results of the units that worker blockIdx.x has the first tile of, joined.  A work-group has one row (grid y),
+// The partial results of the units that worker blockIdx.y has the first tile of, joined.  A work-group has one row (grid x),
 // PAR = 1024 / D groups of D / 4 threads that share the pieces, 64 at a time: a piece's maximum and sum in a lane.
 template <int D>
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedFwdArgs a, const PagedSlots<elem> s, const int R)
 {
     constexpr int kCols = D / 4, PAR = 256 / kCols;
     __shared__ f32x4 sum[PAR][kCols];
-    const PagedJoin j = s.join[blockIdx.x];
-    const int tid = threadIdx.x, l = tid & 63, c = tid % kCols, p = tid / kCols, r = blockIdx.y;
+    const PagedJoin j = s.join[blockIdx.y];
+    const int tid = threadIdx.x, l = tid & 63, c = tid % kCols, p = tid / kCols, r = blockIdx.x;
     if (j.pieces == 0 || r >= j.rows) return;
-    auto at = [&](int i) { return (2 * (int64_t)(blockIdx.x + i) + (i == 0)) * R + r; };
+    auto at = [&](int i) { return (2 * (int64_t)(blockIdx.y + i) + (i == 0)) * R + r; };
     const bool mine = 4 * c < a.Dr;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     float top = kJoinMinusHuge, all = 0.f;
@@ -547,7 +547,7 @@ static int launch_decode_t(const PagedFwdArgs &a, int max_rows, int workers, hip
     } else {
         hipLaunchKernelGGL((attn_paged_decode_kernel<D, RB, E8, true>), dim3(workers), dim3(C::kThreads), C::kLds, st, a,
                            max_rows);
-        hipLaunchKernelGGL(attn_paged_join_kernel<D>, dim3(workers, max_rows), dim3(256), 0, st, a,
+        hipLaunchKernelGGL(attn_paged_join_kernel<D>, dim3(max_rows, workers), dim3(256), 0, st, a,
                            PagedSlots<elem>(a.workspace, workers, 16 * RB, D), 16 * RB);
     }
     return hipGetLastError() == hipSuccess ? 0 : -1;
