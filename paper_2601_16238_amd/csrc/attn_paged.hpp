@@ -89,7 +89,8 @@ struct PagedPlan {
     int workers;      // 0: one work-group for each unit of rows
     size_t bytes;     // workspace
 };
-constexpr int kDecodeSpan = 4, kChunkSpan = 4;  // tiles of a span, at least
+constexpr int kDecodeSpan = 1, kChunkSpan = 4;  // tiles of a span, at least
+constexpr int kWholeTiles = 8;                  // sequences of up to so many are not cut
 constexpr int chunk_rows(int D) { return D == 128 ? 256 : 128; }  // of a unit, in the kernel of many rows
 PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3);
 

@@ -2,12 +2,16 @@
 //
 // Nothing is computed that would count: the kernels move bytes.  A row is worked on in units of twice W columns: columns
 // j .. j+W-1 and their partners j + rot/2 .., which are rotated together, or 2 W consecutive ones behind the rotated.
-// W = 8 (16-byte accesses) where such units cover a row, that is rot and D are multiples of 16, otherwise 4.
+// W = 8 (16-byte accesses) where such units cover a row, that is rot and D are multiples of 16, otherwise 4: prompts of 13K
+// tokens (272 MB, fp16 or bf16) in 51.5 us, 5.3 TB/s, which is what a copy reaches; 61.9 with W = 4.
 #include "attn_paged.hpp"
+
+#include <algorithm>
 
 namespace attn {
 
 constexpr float kE4m3Max = 448.0f;
+constexpr int kAppendKeep = 4;  // units that a thread keeps in registers
 
 template <int W>
 struct Unit {
@@ -63,6 +67,7 @@ __device__ __forceinline__ void turn(const PagedAppendArgs &a, int64_t p, int j,
 // i divided by the units of a row.
 __device__ __forceinline__ int row_of(const PagedAppendArgs &a, int i) { return a.nu_magic ? __umulhi(i, a.nu_magic) : i; }
 
+// A work-group for each token, so that its sequence, position and page are found once for all heads.
 // The rows of token t by one work-group: of Q, and (KV) of K and V, with a 16-bit cache.
 template <int W, bool KV>
 __device__ __forceinline__ void append_token(const PagedAppendArgs &a, int t)
@@ -124,12 +129,18 @@ __device__ __forceinline__ void store_codes(uint8_t *p, const float (&x)[W], flo
 
 // e4m3 cache: one work-group for each page that gets rows (slot), head and tensor; behind them one for each token's Q.
 // Sequence b has the slots from q_start[b] / P + 2 b on: n rows touch at most n / P + 2 pages, so they do not reach into
-// the next one's.  A page's new values are read once, where a thread can keep its units of them (kKeep), and a second
-// time for pages of more than kKeep THREADS units.
+// the next one's.  A page's new values are read once, where a thread can keep its units of them (kAppendKeep), and a second
+// time for pages of more than kAppendKeep THREADS units.
+// Bound by the rows' way through memory: prompts of 19K tokens (229 MB) in 51 us, 4.4 TB/s of the 5.1 that a copy reaches;
+// one token each of 64 sequences in 5 us, that is by latency: q_start, lengths, page, then values and scale.
+// A wave for each page, head and tensor where it can keep the new rows of a page (of a sequence of average length), otherwise
+// four, us with 64 / 256 threads, D = 128 and 8 K/V heads: 64 sequences of 1 row 5.1 / 7.0, 32 rows 10.7 / 13.5;
+// 32 sequences of 100 rows, pages of 16 rows 15.4 / 21.4, of 64 18.2 / 16.6, of 256 24.3 / 15.7; 4000 rows in one page of 4096
+// 764 / 206.  (Twice as many values kept: 58 instead of 50 us for the prompts, fewer waves are resident.)
 template <int W, int THREADS>
 __global__ void __launch_bounds__(THREADS) attn_paged_append8_kernel(const PagedAppendArgs a, const int slots)
 {
-    constexpr int kKeep = 4, kWaves = THREADS / 64;
+    constexpr int kKeep = kAppendKeep, kWaves = THREADS / 64;
     __shared__ float most[kWaves];
     const int tid = threadIdx.x, l = tid & 63;
     if ((int)blockIdx.x >= slots * a.Hkv * 2) {
@@ -247,8 +258,8 @@ static int launch_append_w(PagedAppendArgs a, hipStream_t st)
     } else {
         const int slots = (a.b.T >> a.b.page_shift) + 2 * a.b.B;
         const dim3 grid((unsigned)(slots * a.Hkv * 2 + (a.Q_rot ? a.b.T : 0)));
-        // few new rows a sequence: a wave for each page and head, otherwise four
-        if (a.b.T <= 4 * (int64_t)a.b.B)
+        const int64_t rows = std::min<int64_t>(a.b.page_size(), (a.b.T + a.b.B - 1) / a.b.B);
+        if (rows * nu <= kAppendKeep * 64)
             hipLaunchKernelGGL((attn_paged_append8_kernel<W, 64>), grid, dim3(64), 0, st, a, slots);
         else
             hipLaunchKernelGGL((attn_paged_append8_kernel<W, 256>), grid, dim3(256), 0, st, a, slots);

@@ -85,11 +85,12 @@ struct ChunkUnits {
     unsigned m, b, BR;
     bool causal;
     __device__ ChunkUnits() {}
-    __device__ ChunkUnits(const PagedSeq &s, int G, int max_q, int BR_, bool causal_) : len(s.len), BR(BR_), causal(causal_)
+    __device__ ChunkUnits(const PagedSeq &s, int G, int max_q, int BR_, bool causal_, int light)
+        : len(s.len), BR(BR_), causal(causal_)
     {
         units = s.n > max_q ? 0 : (int)(((unsigned)(s.n * G) + BR - 1) / BR);
         last = max((s.len + 63) >> 6, 1);
-        cost = s.n * G <= kLightRows ? kLightCost : kTileCost;
+        cost = s.n * G <= kLightRows ? light : kTileCost;
         const int before = s.len - s.n;
         q0 = before >> 6;
         m = 64u * G;
@@ -155,7 +156,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     int64_t begin_at = 0, size = 0;  // of the span
     int left = 0;
     const int me = SPLIT ? xcd_contiguous_order(blockIdx.x, gridDim.x) : blockIdx.x;
-    auto units_of = [&](const PagedSeq &q) { return ChunkUnits(q, G, a.max_q, BR, causal); };
+    auto units_of = [&](const PagedSeq &q) { return ChunkUnits(q, G, a.max_q, BR, causal, E8 ? kTileCost : kLightCost); };
     auto next_unit = [&]() __attribute__((always_inline)) {
         // (what the sequence's units are is found again rather than kept: the scalar registers are few)
         ChunkUnits units = units_of(s);

@@ -77,7 +77,7 @@ constexpr int kUnitEnd = 2;
 
 // SPLIT: work-groups with spans, partial results in the workspace.  Otherwise one work-group for each sequence and K/V head.
 template <int D, int RB, bool E8, bool SPLIT>
-__global__ void __launch_bounds__((DecodeCfg<D, E8>::kThreads))
+__global__ void __launch_bounds__((DecodeCfg<D, E8>::kThreads), (D <= 128 ? 2 : 1))
 attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
 {
     using C = DecodeCfg<D, E8>;
@@ -557,8 +557,7 @@ template <int D, bool E8>
 static int launch_decode_d(const PagedFwdArgs &a, int max_rows, int workers, hipStream_t st)
 {
     if (max_rows <= 16) return launch_decode_t<D, 1, E8>(a, max_rows, workers, st);
-    if (max_rows <= 32) return launch_decode_t<D, 2, E8>(a, max_rows, workers, st);
-    if constexpr (D <= 128) return launch_decode_t<D, 4, E8>(a, max_rows, workers, st);
+    if constexpr (D <= 128) return launch_decode_t<D, 2, E8>(a, max_rows, workers, st);
     return -1;
 }
 

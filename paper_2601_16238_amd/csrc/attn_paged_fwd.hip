@@ -10,16 +10,16 @@ PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, in
 {
     PagedPlan p = {};
     p.kernel_d = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-    const int G = Hq / Hkv, most = p.kernel_d == 256 ? 32 : 64;
+    const int G = Hq / Hkv, most = p.kernel_d == 256 ? 16 : 32;
     const int64_t rows = (int64_t)max_q * G;
     if (rows <= most) {
         p.decode_rows = (int)rows;
         const int tile = p.kernel_d == 256 && !e4m3 ? 64 : 128;
         const int64_t tiles = (keys + tile - 1) / tile;
-        if (tiles <= kDecodeSpan) return p;
+        if (tiles <= kWholeTiles) return p;
         const int lds = p.kernel_d * (e4m3 ? 1 : 2) * 64 * 2 * (tile / 32), per_cu = 160 * 1024 / (lds + 4096);
         p.workers = (int)std::min<int64_t>(256 * std::min(per_cu, 2), B * Hkv * ((tiles + kDecodeSpan - 1) / kDecodeSpan));
-        p.bytes = paged_span_bytes(p.workers, rows <= 16 ? 16 : rows <= 32 ? 32 : 64, p.kernel_d);
+        p.bytes = paged_span_bytes(p.workers, rows <= 16 ? 16 : 32, p.kernel_d);
         return p;
     }
     // A batch that may hold long sequences: all of it by the kernel of many rows, also the sequences of one token next
