@@ -91,7 +91,8 @@ int attn_paged_append_f16(const void *K, const void *V, const void *Q, void *Q_r
 /*
  * Attention of the batch's rows over the cache: O (of Q's type) and LSE, fp32 [T][Hq] contiguous, natural
  * logarithm.  A row that sees no key gets O = 0 and LSE = -infinity.
- * (T Hq/Hkv / 128 + B) (table_width page_size / 32 + 16), what spreading the work counts with, has to be an int32.
+ * (T Hq/Hkv / 128 + B) Hkv (table_width page_size / 32 + 16), what spreading the work counts with, has to be an int32:
+ * with 32 query and 8 K/V heads, a prompt of half a million tokens in one call.
  *   workspace: NULL (every row's keys are worked through by one work-group), or 256-byte aligned and of at least
  *     attn_fwd_paged_workspace_bytes: work over many keys is then spread over the whole chip.  Its contents are not
  *     read before they are written.

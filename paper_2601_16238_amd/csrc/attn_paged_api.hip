@@ -91,7 +91,9 @@ int fwd_impl(const void *Q, const void *K_cache, const void *V_cache, const floa
     if (p->max_q < 1 && p->T > 0) return ATTN_ERR_SHAPE;
     // (what all tiles of keys together count in the spans of the work-groups)
     const int64_t units = (int64_t)p->T * (p->Hq / p->Hkv) / 128 + p->B, keys = (int64_t)p->table_width * p->page_size;
-    if (units * (keys / 32 + 16) > std::numeric_limits<int32_t>::max()) return ATTN_ERR_SHAPE;
+    if (units > std::numeric_limits<int32_t>::max() ||
+        units * (keys / 32 + 16) > std::numeric_limits<int32_t>::max() / p->Hkv)
+        return ATTN_ERR_SHAPE;
     if (!std::isfinite(p->scale) || !(p->scale > 0.0f)) return ATTN_ERR_SCALE;
     if (p->T == 0 || p->B == 0) return ATTN_OK;
     if (!Q || !K_cache || !V_cache || !page_table || !q_start || !kv_lens || !O || !LSE) return ATTN_ERR_NULL;

@@ -87,6 +87,15 @@ def test_bad_parameters_of_one_call():
     assert append(params(kv_stride_h=-64)) == binding.ATTN_ERR_STRIDE
 
 
+def test_heads_times_keys():
+    """What the spans of all heads count with is an int32: the longest table with 64 K/V heads is not."""
+    p = params(T=1, B=1, Hq=64, Hkv=64, max_q=1, page_size=4096, table_width=1 << 18, table_stride=1 << 18,
+               q_stride_t=64 * 64, out_stride_t=64 * 64, cache_stride_h=4096 * 64, cache_stride_p=64 * 4096 * 64)
+    for q in (1, 64):
+        p.T = p.max_q = q
+        assert fwd(p) == fwd(p, "attn_fwd_paged_f16") == binding.ATTN_ERR_SHAPE
+
+
 def test_pointers():
     for n in ("Q", "K", "V", "table", "q_start", "kv_lens", "O", "LSE"):
         assert fwd(params(), **{n: None}) == binding.ATTN_ERR_NULL
