@@ -89,8 +89,13 @@ struct PagedPlan {
     int workers;      // 0: one work-group for each unit of rows
     size_t bytes;     // workspace
 };
-constexpr int kDecodeSpan = 1, kChunkSpan = 4;  // tiles of a span, at least
-constexpr int kWholeTiles = 8;                  // sequences of up to so many are not cut
+// Tiles of a span, at least: shorter ones cost more in the join than they save.  us with 1 / 2 / 4, few rows: 10.9 / 12.3 /
+// 15.1 (one sequence of 1000 keys), 12.5 / 13.7 / 16.0 (4000); with 2 / 4 / 8, many rows: 26.9 / 25.5 / 28.4 (128 new
+// tokens after 1000 keys).
+constexpr int kDecodeSpan = 1, kChunkSpan = 4;
+// Few rows: a table of up to so many tiles is not cut, and nothing joined: us uncut / cut, 600 keys: 8.2 / 10.4 (one sequence),
+// 29.7 / 32.1 (64); 1000 keys: 11.1 / 11.0 (one; e4m3 11.9 / 10.3), 44.7 / 47.9 (64).
+constexpr int kWholeTiles = 8;
 constexpr int chunk_rows(int D) { return D == 128 ? 256 : 128; }  // of a unit, in the kernel of many rows
 PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3);
 

@@ -5,13 +5,20 @@
 // 32 of them.  S^T = K Q^T and O^T += V^T P^T by 32x32x16 MFMA with the scores of a query in one lane.  A
 // step forms the scores of 32 keys, the probabilities of the 32 before them and the products with V of the 32 before
 // those: three independent pieces of work in one block of code, so that the matrix pipe and the vector ALU overlap inside
-// a wave.  K and V tiles reach LDS row-major, two buffers each: two steps share a pair of tiles of 64 keys, K's 32 keys
+// a wave.  K and V tiles reach LDS row-major, two or three buffers each: two steps share a pair of tiles of 64 keys, K's 32 keys
 // ahead of the probabilities and V's 32 behind.  16-bit tiles come by direct transfers, 16 rows (of one page) to a buffer
 // resource; slots behind the last key, pages that are none and columns that do not exist read as zero.  e4m3 tiles
 // pass through registers, where they are converted once for all waves: K exactly, V with its power of two; what is
 // left of V's scale is added to the exponent of the probabilities and taken out of their sums.
 //
 // Work is cut into equal spans of tiles, as for few rows (attn_paged_decode.hip).
+//
+// Bound by the products and the exponentials beside them: a unit's tile of 256 rows and 64 keys takes 2.1 us of a compute unit
+// (2.2 with e4m3), 1.0 PFLOP/s of the 1.2 that a large product reaches.  Prompts of 16.6K tokens (567 GFLOP) in 600 us and 15
+// for the join, 512 tokens after 3584 keys (32 GFLOP) in 45 + 9, half of it beginnings and ends: a span's place, the first
+// tiles' way and the partial results, 128 KB each.
+// Eight waves of 32 rows a work-group with D = 128, so that a tile's way from L2 serves 256 rows: prompts 619 us, 798 with
+// four; 16-bit tiles in three buffers: 15 sequences of one token beside a chunk 86 us, 95 with two, prompts the same.
 #include "attn_paged.hpp"
 
 #include <type_traits>
@@ -73,8 +80,11 @@ __device__ __forceinline__ int64_t floor_sum(unsigned n, unsigned m, unsigned a,
     }
     return sum;
 }
-// What spans count: a tile as 2, or as 1 where one or two waves have rows (sequences of few rows next to long ones), and the
-// beginning and end of a unit, where its rows come and go, as 6.
+// What spans count: a tile as 2, or, 16-bit, as 1 where one or two waves have rows (sequences of few rows next to long ones),
+// and the beginning and end of a unit, where its rows come and go, as 6.  15 sequences of one token beside a chunk: 86 us with
+// such tiles as 1, 94 as 2; e4m3, whose tiles wait for the codes' way to the registers whatever the rows are, 111 as 1
+// and 98 as 2.  The ends as 0 / 4 / 6 / 8: prompts 837 / 755 / 725 / 711 us when they took longest, 665 / - / 657 / 655
+// since their rows are requested together; as 10: mixed batches 98 -> 101.
 constexpr int kTileCost = 2, kLightCost = 1, kLightRows = 64, kChunkEnd = 6;
 // The units of a sequence and K/V head, unit rt with the rows rt BR .. of the sequence's n G, and their tiles of 64 keys:
 // those that its last row sees (none: one, in which nothing is seen).  Under a causal mask these are
@@ -129,7 +139,9 @@ struct ChunkUnits {
     }
 };
 
-constexpr float kChunkOverflow = 1024.0f;  // a lane's sum of a score block above this moves the reference maximum
+// A lane's sum of the probabilities of its 16 keys above this moves the reference maximum: until then they stay inside the exponents
+// of either type (fp16: up to 2^15), so that rounding them to it costs the same; sums and products are fp32.
+constexpr float kChunkOverflow = 1024.0f;
 constexpr float kChunkMinusHuge = -1.0e30f;
 
 template <int D, bool E8, bool SPLIT>
@@ -233,8 +245,8 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
     const uint32_t voff = L::lane_offset(l, row_bytes, Dr, kPast);
     // Set j: the groups 4 j + 2 .. 4 j + 5 of 16 keys each, counted from the unit's first key that the span has; they are
     // K's tile j and V's tile j + 1.  A wave fetches rows of one group, `own`, and tells the others what its
-    // scores are multiplied with, what is added to the exponents of its probabilities (minus infinity: no page, or behind the last key) and what their
-    // sum is multiplied with.
+    // scores are multiplied with, what is added to the exponents of its probabilities (minus infinity: no page, or behind
+    // the last key) and what their sum is multiplied with.
     const int own = w * C::kWaveRows / 16, own_row = w * C::kWaveRows % 16;
     struct Const { float c, rest, inv, unused; };
     constexpr int kSets = 4;
@@ -618,8 +630,8 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             for (int j = 0; j < 2; ++j) {
                 const int in = w * 32 + 16 * j + l / 4, t = over_group(e.base_head + in);
                 store[j] = in < e.rows;
-                out[j] = a.O + (e.first + e.base_tok + t) * a.out_stride_t + (e.h * G + e.base_head + in - t * G) * a.out_stride_h +
-                         l % 4 * 8;
+                out[j] = a.O + (e.first + e.base_tok + t) * a.out_stride_t +
+                         (e.h * G + e.base_head + in - t * G) * a.out_stride_h + l % 4 * 8;
             }
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
