@@ -89,12 +89,15 @@ struct PagedPlan {
     int workers;      // 0: one work-group for each unit of rows
     size_t bytes;     // workspace
 };
-// Tiles of a span, at least: shorter ones cost more in the join than they save.  us with 1 / 2 / 4, few rows: 10.9 / 12.3 /
-// 15.1 (one sequence of 1000 keys), 12.5 / 13.7 / 16.0 (4000); with 2 / 4 / 8, many rows: 26.9 / 25.5 / 28.4 (128 new
-// tokens after 1000 keys).
-constexpr int kDecodeSpan = 1, kChunkSpan = 4;
-// Few rows: a table of up to so many tiles is not cut, and nothing joined: us uncut / cut, 600 keys: 8.2 / 10.4 (one sequence),
-// 29.7 / 32.1 (64); 1000 keys: 11.1 / 11.0 (one; e4m3 11.9 / 10.3), 44.7 / 47.9 (64).
+// Tiles of a span, at least (every piece that the join counts has to have one).  us with 1 / 2 / 4, few rows: 10.9 / 12.3 /
+// 15.1 (one sequence of 1000 keys), 12.5 / 13.7 / 16.0 (4000); many rows: 16.1 / 19.1 / 25.6 (two sequences of up to 11 rows
+// and 807 keys, D = 192), 26.6 / 25.6 / 27.7 (5 of up to 206 and 780), 28.1 / 25.7 / 24.6 (one of 104 and 2089); batches drawn
+// over the whole range 1 % faster with 2 than with 1 and 4 % than with 4.
+constexpr int kDecodeSpan = 1, kChunkSpan = 2;
+// A table of up to so many tiles is not cut, and nothing joined.  us uncut / cut, few rows, 600 keys: 8.2 / 10.4 (one sequence),
+// 29.7 / 32.1 (64); 1000 keys: 11.1 / 11.0 (one; e4m3 11.9 / 10.3), 44.7 / 47.9 (64).  Many rows, 310 keys: 25.8 / 36.0 (5
+// sequences of up to 273 rows, D = 192), 9.8 / 18.5 (7 of up to 212); 494 keys: 11.2 / 10.4 (one of 19); beyond, 676 keys:
+// 26.8 / 19.1 (22 of up to 150).
 constexpr int kWholeTiles = 8;
 constexpr int chunk_rows(int D) { return D == 128 ? 256 : 128; }  // of a unit, in the kernel of many rows
 PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, int64_t keys, bool e4m3);

@@ -33,6 +33,7 @@ PagedPlan paged_plan(int64_t T, int64_t B, int Hq, int Hkv, int D, int max_q, in
     const int unit = chunk_rows(p.kernel_d);
     // (D = 64: two work-groups a compute unit, prompts 445 us; with one 554)
     const int64_t units = (T * G / unit + std::min(B, T)) * Hkv, tiles = (keys + 63) / 64;
+    if (tiles <= kWholeTiles) return p;
     p.workers = (int)std::min<int64_t>(p.kernel_d == 64 ? 512 : 256, units * ((tiles + kChunkSpan - 1) / kChunkSpan));
     p.bytes = paged_span_bytes(p.workers, unit, p.kernel_d);
     return p;
