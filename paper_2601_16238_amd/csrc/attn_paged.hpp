@@ -128,24 +128,32 @@ __device__ __forceinline__ int paged_seq_of(const PagedBatch &a, int t)
     return a.B;
 }
 
-// Inclusive sum over a work-group's threads, and over all of them.
+// Sum of two numbers that are not negative, at most lim.
+__device__ __forceinline__ int add_up_to(int a, int b, int lim) { return (int)min((unsigned)a + (unsigned)b, (unsigned)lim); }
+
+// Sum over a work-group's threads up to this one, over those before it, and over all of them, each at most lim.
 template <int NW>
-__device__ __forceinline__ int block_scan(int v, int *lds, int &all)
+__device__ __forceinline__ int block_scan(int v, int lim, int *lds, int &before, int &all)
 {
     const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const int x = __shfl_up(v, d);
-        if (l >= d) v += x;
+        if (l >= d) v = add_up_to(v, x, lim);
     }
+    before = __shfl_up(v, 1);
+    if (l == 0) before = 0;
     __syncthreads();
     if (l == 63) lds[w] = v;
     __syncthreads();
     all = 0;
 #pragma unroll
     for (int i = 0; i < NW; ++i) {
-        if (i < w) v += lds[i];
-        all += lds[i];
+        if (i < w) {
+            v = add_up_to(v, lds[i], lim);
+            before = add_up_to(before, lds[i], lim);
+        }
+        all = add_up_to(all, lds[i], lim);
     }
     return v;
 }
@@ -167,6 +175,8 @@ __device__ __forceinline__ PagedSeq paged_seq_scalar(const PagedBatch &a, int b)
 
 // The span of worker w of `workers`: `tiles(seq)` are those of a sequence with one head, of which there are `heads`.
 // Where the span begins: sequence b, and how many tiles lie in front of that sequence (all heads).
+// The sums end at what an int32 holds.  Row ranges that lie apart never get there (the host has checked), others, which
+// are an error of the caller's, do not lead outside the buffers that way: a sequence that is found has its tiles.
 struct PagedSpan {
     int64_t begin, front, size;
     int left, b;  // tiles of the span (0: none)
@@ -184,6 +194,7 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedBatch &a, int heads, 
 {
     const int tid = threadIdx.x, l = tid & 63, B = a.B;
     PagedSpan s = {};
+    const int lim = 0x7fffffff / heads;
     auto cut = [&](int64_t total) __attribute__((always_inline)) {
         s.size = max((int64_t)least, div_up(total, workers));
         s.begin = w * s.size;
@@ -197,47 +208,47 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedBatch &a, int heads, 
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const int x = __shfl_up(sum, d);
-            if (l >= d) sum += x;
+            if (l >= d) sum = add_up_to(sum, x, lim);
         }
         cut((int64_t)__builtin_amdgcn_readlane(sum, 63) * heads);
         if (s.left == 0) return s;
         s.b = __builtin_ctzll(__builtin_amdgcn_ballot_w64((int64_t)sum * heads > s.begin));
-        s.front = (int64_t)__builtin_amdgcn_readlane(sum - mine, s.b) * heads;
+        s.front = s.b ? (int64_t)__builtin_amdgcn_readlane(sum, s.b - 1) * heads : 0;
         s.seq.first = __builtin_amdgcn_readlane(q.first, s.b);
         s.seq.n = __builtin_amdgcn_readlane(q.n, s.b);
         s.seq.len = __builtin_amdgcn_readlane(q.len, s.b);
         s.tiles = __builtin_amdgcn_readlane(mine, s.b);
         return s;
     }
-    int64_t total = 0;
-    int mine = 0, sum = 0, all = 0;
+    int total = 0, front = 0, sum = 0, before = 0, all = 0;
+    auto sums = [&](int b0) __attribute__((always_inline)) {
+        sum = block_scan<NW>(b0 + tid < B ? tiles(paged_seq(a, b0 + tid)) : 0, lim, lds, before, all);
+    };
     for (int b0 = 0; b0 < B; b0 += NW * 64) {
-        mine = b0 + tid < B ? tiles(paged_seq(a, b0 + tid)) : 0;
-        sum = block_scan<NW>(mine, lds, all);
-        total += all;
+        sums(b0);
+        total = add_up_to(total, all, lim);
     }
-    cut(total * heads);
+    cut((int64_t)total * heads);
     if (s.left == 0) return s;
     // (one round: its sums are still there)
     for (int b0 = 0; b0 < B; b0 += NW * 64) {
-        if (B > NW * 64) {
-            mine = b0 + tid < B ? tiles(paged_seq(a, b0 + tid)) : 0;
-            sum = block_scan<NW>(mine, lds, all);
-        }
-        if ((s.front + all) * heads > s.begin) {
+        if (B > NW * 64) sums(b0);
+        const int behind = add_up_to(front, all, lim);
+        if ((int64_t)behind * heads > s.begin) {
             __syncthreads();
-            if ((s.front + sum) * heads > s.begin && (s.front + sum - mine) * heads <= s.begin) {
+            const int from = add_up_to(front, before, lim);
+            if ((int64_t)add_up_to(front, sum, lim) * heads > s.begin && (int64_t)from * heads <= s.begin) {
                 lds[0] = b0 + tid;
-                lds[1] = sum - mine;
+                lds[1] = from;
             }
             __syncthreads();
             s.b = __builtin_amdgcn_readfirstlane(lds[0]);
-            s.front = (s.front + __builtin_amdgcn_readfirstlane(lds[1])) * heads;
+            s.front = (int64_t)__builtin_amdgcn_readfirstlane(lds[1]) * heads;
             s.seq = paged_seq_scalar(a, s.b);
             s.tiles = __builtin_amdgcn_readfirstlane(tiles(s.seq));
             return s;
         }
-        s.front += all;
+        front = behind;
     }
     return s;
 }

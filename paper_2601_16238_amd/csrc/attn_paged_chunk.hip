@@ -668,7 +668,7 @@ attn_paged_chunk_kernel(const PagedFwdArgs a, const PagedSlots<elem> slots)
             }
             if (e.from_start && tid == 0) {
                 const int64_t last = begin_at + e.begins + e.last;  // where the unit's last tile begins
-                slots.join[me] = PagedJoin{e.first, e.h, e.row0, e.rows, (int)(last / size) - me + 1};
+                slots.join[me] = PagedJoin{e.first, e.h, e.row0, e.rows, min((int)(last / size), (int)gridDim.x - 1) - me + 1};
             }
         }
         if (!more) return;

@@ -389,7 +389,8 @@ attn_paged_decode_kernel(const PagedFwdArgs a, const int max_rows)
         if (SPLIT && from_start && !to_end && tid == 0) {
             // the unit's last tile lies u.tiles - u.t - 1 behind this one, the span's last
             const int64_t last = span.begin + span.left - 1 + (u.tiles - 1 - u.t);
-            slots.join[blockIdx.x] = PagedJoin{u.first, u.h, 0, rows, (int)(last / span.size) - (int)blockIdx.x + 1};
+            slots.join[blockIdx.x] = PagedJoin{u.first, u.h, 0, rows,
+                                                   min((int)(last / span.size), (int)gridDim.x - 1) - (int)blockIdx.x + 1};
         }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {

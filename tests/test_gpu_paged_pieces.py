@@ -92,3 +92,22 @@ def test_replayed_graph_of_append_and_attention(e4m3):
         if e4m3:
             b.scale = [g["ks"].cpu(), g["vs"].cpu()]
         check_attention(b, o, lse, True, scale=0.1)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["16", "e4m3"])
+@pytest.mark.parametrize("B", [7, 600])
+def test_row_ranges_that_overlap(B, e4m3):
+    """An error of the caller's, which stays inside the buffers: rows of nobody keep what they hold."""
+    b = Batch([(1, 30 + 13 * i % 700) for i in range(B)], 4, 2, 64, 16, e4m3=e4m3, seed=B, behind=4, table_pad=80)
+    g = b.on_gpu()
+    for q_start in ([i % 2 * B for i in range(B + 1)], [B] + [0] * B, [max(0, B - 3 * i) for i in range(B + 1)],
+                    [-5] * B + [B]):
+        g["q_start"] = torch.tensor(q_start, dtype=torch.int32, device="cuda")
+        for max_q in (1, None):
+            O, LSE = torch.full_like(g["q"], 3.0), torch.full(g["q"].shape[:2], 3.0, device="cuda")
+            call(g, 0.1, True, max_q=max_q, O=O, LSE=LSE)
+            torch.cuda.synchronize()
+            assert (O[B:] == 3).all() and (LSE[B:] == 3).all()
+    g["q_start"] = b.q_start.cuda()
+    o, lse = call(g, 0.1, True, max_q=1)
+    check_attention(b, o, lse, True, scale=0.1)
