@@ -72,8 +72,8 @@ def attn_fwd_paged(Q, K_cache, V_cache, page_table, q_start, kv_lens, scale, cau
                    max_q=None, O=None, LSE=None, workspace=None, split=True, stream=None):
     """O [T,Hq,D], LSE [T,Hq] = attention of the batch's rows Q over the caches; batch and caches as in
     attn_paged_append.  With causal=True the row at position p sees keys 0 .. p, otherwise all kv_lens[b]; a row that
-    sees none gets O = 0 and LSE = -inf.  max_q: no sequence has more rows (1 when decoding; a call without it cannot
-    know that and also enqueues the kernels for long sequences); rows of one that has more are left as they were, as
+    sees none gets O = 0 and LSE = -inf.  max_q: no sequence has more rows (1 when decoding; without it a
+    call counts with sequences of many rows and takes the kernel for those); rows of one that has more are left as they were, as
     are those behind the last sequence.  `split=False` passes no workspace, which leaves every row's keys to one
     work-group.  e4m3 caches with their scales (any fp32 scale that is 0 or positive and normal)."""
     return _call(marshal().attn_fwd_paged, stream, Q, K_cache, V_cache, page_table, q_start, kv_lens, float(scale),
